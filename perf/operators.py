@@ -183,14 +183,16 @@ def prepare(case, seed):
             total += (s + _BLOCK - 1) // _BLOCK * _BLOCK        # tensors of one allocation, each on a block boundary
         blocks = torch.tensor([(s + _BLOCK - 1) // _BLOCK for s in sizes], device=dev)
         last = torch.tensor([o + s for o, s in zip(offs, sizes)], device=dev)
-        # which elements of the allocation belong to a tensor
+        # which elements of the allocation belong to a tensor, and where in it they are
         live = torch.arange(total, device=dev) < torch.repeat_interleave(last, blocks * _BLOCK)
+        if case["bits"] == 8:
+            st["index"] = torch.arange(total, device=dev) - torch.repeat_interleave(torch.tensor(offs, device=dev), blocks * _BLOCK)
         st["p"] = 0.02 * normal(total) * live
         st["g"] = (1e-3 * normal(total) * live).to(_TYPES[case["gtype"]])
         m = 3e-4 * normal(total) * live
         r = (1e-3 * (0.05 + normal(total).abs())) * live
         if case["bits"] == 8:
-            (st["m"], st["s_m"]), (st["v"], st["s_v"]) = _encode_states(m.view(-1, _BLOCK), r.view(-1, _BLOCK))
+            (st["m"], st["s_m"]), (st["v"], st["s_v"]) = _encode_states(m.view(-1, _BLOCK), r.view(-1, _BLOCK), 32768, 32768)
         else:
             st["m"], st["v"] = m, r * r
         st["step"] = torch.full((1,), _STEP, dtype=torch.int32, device=dev)
@@ -249,18 +251,23 @@ def _e4m3_units(x):
     return s, e, t * _pow2(3 - e)
 
 
-def _encode_states(m, r):
-    """Codes (uint8) and block exponents (int8) of the 8-bit states: the first moment and the root of the second.  Both
-    round pseudo-stochastically (to nearest, a state that changes by a thousandth a step would stand still): the root by
-    its own discarded bits, and never to zero; the moment by those of the root, because nine tenths of a short number
-    repeat the same four bits."""
+def _encode_states(m, r, t_m, t_r):
+    """Codes (uint8) and block exponents (int8) of the 8-bit states, the first moment and the root of the second: rounded up
+    where 16 fraction bits and 16 random ones carry.  The root does not round to zero."""
     (s_m, e_m, u_m), (s_r, e_r, u_r) = _e4m3_units(m), _e4m3_units(r)
-    v = torch.floor(u_r * 65536.0).to(torch.int32)
-    q_m = (torch.floor(u_m * 65536.0).to(torch.int32) + ((v & 255) << 8 | ((v >> 8) & 255))) >> 16
-    q_r = torch.maximum(_round_units(u_r, 0).to(torch.int32), (r > 0).to(torch.int32))
+    q_m = (torch.floor(u_m * 65536.0).to(torch.int32) + t_m) >> 16
+    q_r = torch.maximum((torch.floor(u_r * 65536.0).to(torch.int32) + t_r) >> 16, (r > 0).to(torch.int32))
     code_m = ((e_m + 6) << 3) + q_m + torch.where(m < 0, 128, 0)
     code_r = ((e_r + 6) << 3) + q_r
     return [(c.to(torch.uint8).view(-1), s.to(torch.int8).view(-1)) for c, s in ((code_m, s_m), (code_r, s_r))]
+
+
+def _random_bits(index, step):
+    """32 bits for an element of a tensor in a step: a mixing function of both (multiplications and shifts mod 2^32)."""
+    x = index ^ ((step.long() * 0x9E3779B9) & 0xFFFFFFFF)
+    x = ((x ^ (x >> 16)) * 0x7FEB352D) & 0xFFFFFFFF
+    x = ((x ^ (x >> 15)) * 0x846CA68B) & 0xFFFFFFFF
+    return x ^ (x >> 16)
 
 
 def _decode_e4m3(code, s):
@@ -339,7 +346,8 @@ def _plain(st):
     p.copy_(p * (1 - _LR * st["decay"]) - (_LR / c1).float() * (m / (v.sqrt() * (1 / c2.sqrt()).float() + _EPS)))
     out = {"p": st["p"]}
     if eight:
-        for name, (code, s) in zip("mv", _encode_states(m, v.sqrt())):
+        bits = _random_bits(st["index"], st["step"]).view(-1, _BLOCK)
+        for name, (code, s) in zip("mv", _encode_states(m, v.sqrt(), (bits >> 16).to(torch.int32), (bits & 65535).to(torch.int32))):
             st[name].copy_(code)
             st["s_" + name].copy_(s)
             out[name] = _decode_e4m3(code, s).to(torch.bfloat16).view(-1)
@@ -429,19 +437,25 @@ def _exact_scale(top, integer_bits):
     return torch.where(top > 0, torch.exp2(s.clamp(min=-100.0)), torch.ones_like(top))
 
 
-def _exact_states(m, r):
-    """What the 8-bit states stand for: four significant bits of a value over its block's scale, steps of 2^-9 below 2^-6."""
+def _exact_states(m, r, index, step):
+    """What the 8-bit states stand for: four significant bits of a value over its block's scale, steps of 2^-9 below 2^-6,
+    rounded up with the probability of the remainder (by 16 random bits)."""
+    x = index ^ (step * 0x9E3779B9 % 2 ** 32)
+    for shift, factor in ((16, 0x7FEB352D), (15, 0x846CA68B)):
+        x = x ^ torch.div(x, 2 ** shift, rounding_mode="floor")
+        # (times the factor's halves, to stay within 64 bits)
+        x = (x * (factor % 65536) + ((x * (factor // 65536)) % 65536) * 65536) % 2 ** 32
+    x = x ^ torch.div(x, 65536, rounding_mode="floor")
     found = []
-    for x in (m.view(-1, _BLOCK), r.view(-1, _BLOCK)):
-        scale = _exact_scale(x.abs().amax(1, keepdim=True), 8)
-        t = x.abs() / scale
-        step = _exact_scale(t, 4).clamp(min=2.0 ** -9)
-        found.append((torch.where(t > 0, t / step, t), torch.where(t > 0, step, torch.full_like(step, 2.0 ** -9)) * scale))
-    (n_m, unit_m), (n_r, unit_r) = found
-    drawn = (n_r - n_r.floor()) * 256
-    threshold = ((drawn - drawn.floor()) * 256).floor() / 256 + drawn.floor() / 65536      # the later bits first
-    q_m = ((n_m * 65536).floor() / 65536 + threshold).floor()
-    q_r = torch.maximum(_exact_round(n_r, 0), (n_r > 0).double())
+    for v, draw in ((m, torch.div(x, 65536, rounding_mode="floor")), (r, x % 65536)):
+        v = v.view(-1, _BLOCK)
+        scale = _exact_scale(v.abs().amax(1, keepdim=True), 8)
+        t = v.abs() / scale
+        unit = torch.where(t > 0, _exact_scale(t, 4).clamp(min=2.0 ** -9), torch.full_like(t, 2.0 ** -9))
+        q = ((t / unit * 65536).floor() + draw.view(-1, _BLOCK).double()).div(65536).floor()
+        found.append((q, unit * scale))
+    (q_m, unit_m), (q_r, unit_r) = found
+    q_r = torch.maximum(q_r, (r.view(-1, _BLOCK) > 0).double())
     return (torch.sign(m).view(-1, _BLOCK) * q_m * unit_m).view(-1), (q_r * unit_r).view(-1)
 
 
@@ -509,7 +523,7 @@ def exact(case, seed):
     p = p - _LR * decay * p - _LR * (m / (1 - _BETA1 ** _STEP)) / ((v / (1 - _BETA2 ** _STEP)).sqrt() + _EPS)
     out = {"p": p, "m": m, "v": v}
     if eight:
-        out["m"], out["v"] = _exact_states(m, v.sqrt())
+        out["m"], out["v"] = _exact_states(m, v.sqrt(), st["index"], _STEP)
     if case["w8"]:
         scale = torch.exp2(st["s_w_blocks"].to(d)).expand(-1, _BLOCK).reshape(-1)
         out["w8"] = torch.sign(p) * _exact_round(p.abs() / scale, 1).clamp(max=127) * scale
