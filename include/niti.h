@@ -74,6 +74,17 @@ extern "C" {
 #define NITI_OP_INT_XENT 5    /* dims = {B, N}                    */
 #define NITI_OP_LINEAR_BWD_UPDATE 6 /* dims = {M, N, K}            */
 #define NITI_OP_CONV_WGRAD_UPDATE 7 /* dims as NITI_OP_CONV_FWD    */
+#define NITI_OP_RMSNORM_FWD 8 /* dims = {M, C}                    */
+#define NITI_OP_RMSNORM_BWD 9 /* dims = {M, C}                    */
+#define NITI_OP_QUANTIZE 10   /* dims = {M, C}                    */
+
+/* element types of the float tensors that some calls take */
+#define NITI_F32 0
+#define NITI_BF16 1
+#define NITI_F16 2
+/* 8-bit formats of niti_dequantize() */
+#define NITI_I8 0             /* int8 payload                     */
+#define NITI_E4M3 1           /* sign, 4 exponent bits (bias 7), 3 fraction bits; codes 127 and 255 do not occur */
 
 /* device status bits returned by niti_check() */
 #define NITI_DEV_TIMEOUT 1u      /* a bounded wait inside a kernel gave up (blocks that wait for other blocks of
@@ -82,6 +93,8 @@ extern "C" {
 #define NITI_DEV_XENT_RANGE 4u   /* s_a outside [-22, 24] in niti_int_xent     */
 #define NITI_DEV_BAD_LABEL 8u    /* a label outside [0, N)                     */
 #define NITI_DEV_INTERNAL 32u    /* a consistency check inside a kernel failed: outputs of that call are not exact */
+#define NITI_DEV_BAD_STEP 128u   /* niti_adamw: *step below 1; nothing was updated */
+#define NITI_DEV_NONFINITE 64u   /* a float operand (or what it leads to) is infinite or not a number */
 #define NITI_DEV_ACC_RANGE 16u   /* an int32 accumulator may have wrapped: in a contraction split over
                                   * CTAs the largest partial sums of the splits add up to 2^31 or more */
 
@@ -411,6 +424,79 @@ int niti_maxpool2_fwd_idx(niti_ctx *ctx, void *stream, const int8_t *x, int8_t *
                           int W, int C);
 int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, const uint8_t *idx, int8_t *e_in,
                           int B, int H, int W, int C, int relu);
+
+/* ---- Float tensors at the boundary of the format: the feed-forward block of a transformer --------------------------
+ * A residual stream of float rows (`type`: NITI_F32, NITI_BF16 or NITI_F16) enters the format through a norm, passes
+ * int8 multiplies and comes back through their epilogue.  Float pointers are aligned to their element; rows of whole,
+ * 16-byte aligned vectors are fastest.  M = 0 is a valid call.  Sums, statistics and everything between a load and the
+ * final rounding are float32.
+ *
+ * Rounding a float y to a payload with exponent s.  For a largest magnitude A the exponent is
+ *   s = max(floor(log2 A) - 6, -100),  0 for A = 0,
+ * so that payloads reach 64 .. 127; with u = |y| 2^-s, round_mode 1 gives floor(u + 1/2), round_mode 0 takes 16
+ * fraction bits and adds one to the integer part where their top half is larger than their bottom half (Algorithm 3
+ * with bp = 16); at most 127, sign re-applied.  Pseudo-stochastic rounding draws from discarded bits: a value that
+ * comes straight from a 16-bit type has too few of them, and calls that would round such values refuse it.
+ * Exponents go to s[M], one per row, with row_exponents != 0 (a row is then independent of the others: serving), else to
+ * s[0], one for the tensor (what the backward multiplies can take out of their sums: training).
+ * An infinity or NaN raises NITI_DEV_NONFINITE; its row's (tensor's) exponent is then 121, NaN becomes payload 0 and an
+ * infinity +-127.
+ *
+ * Root-mean-square norm:  h = x + residual (rounded to `type`; without a residual h is x and not written),
+ *   r = 1 / sqrt(mean_c h^2 + eps),  y = round(h r gain).
+ * x, residual, h [M][C]; gain [C] float32; y [M][C] int8; rstd [M] float32 receives r (may be NULL).  h is needed with a
+ * residual, and may be the storage of x or of the residual.  Workspace: NITI_OP_RMSNORM_FWD. */
+int niti_rmsnorm_fwd(niti_ctx *ctx, void *stream, const void *x, const void *residual, const float *gain, void *h,
+                     int8_t *y, int32_t *s_y, float *rstd, int type, int M, int C, int row_exponents, float eps,
+                     int round_mode, void *ws, size_t ws_bytes);
+
+/* Its backward pass, the rounding taken as the identity:  with G = gain dy,
+ *   dx = dh + r G - h r^3 mean_c(G h),   dgain = sum_m dy h r.
+ * dy, h, dh, dx [M][C] of `type`; dh, the gradient that reaches h past the norm, may be NULL (0), and so may dgain [C].
+ * dx is the gradient of x and of the residual; it may be the storage of dy, h or dh.  The sums of dgain are added in a
+ * fixed order.  Workspace: NITI_OP_RMSNORM_BWD. */
+int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, const void *h, const float *gain, const float *rstd,
+                     const void *dh, void *dx, float *dgain, int type, int M, int C, void *ws, size_t ws_bytes);
+
+/* q = round(x) with one exponent per row of C elements, or one.  Workspace: NITI_OP_QUANTIZE. */
+int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t *q, int32_t *s, int type, int M, int C,
+                  int row_exponents, int round_mode, void *ws, size_t ws_bytes);
+
+/* out[i] = value(q[i]) 2^s[i / per], i < n: payloads (NITI_I8) or codes (NITI_E4M3) of n elements, `per` elements for
+ * every exponent (0: one exponent for all); exponents of exponent_bytes = 4 (int32) or 1 (int8). */
+int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, void *out, int format,
+                    int exponent_bytes, int type, int64_t n, int64_t per);
+
+/* One AdamW step over n tensors (a host array that the call reads before it returns; two of them must not share
+ * memory).  With t = *step, the number of this step (device int32, >= 1: a captured graph counts it up between its
+ * replays), and g the gradient times *grad_scale (device float32, NULL: 1):
+ *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps),
+ *   w8 <- floor(|p| 2^-s_w + 1/2), at most 127, sign of p (unless w8 is NULL): the int8 weights that the multiplies read,
+ * with the exponent *s_w that the caller has chosen for the tensor.
+ * state_bits 32: m, v float32 [n].  state_bits 8: m and r = sqrt(v) are bytes in the format NITI_E4M3 with an int8
+ * exponent for every NITI_STATE_BLOCK elements, in s_m and s_v [ceil(n / NITI_STATE_BLOCK)]; fresh states are zero bytes
+ * with zero exponents.  The exponent leaves values of the block in [0, 256); they round stochastically to codes, up where
+ * the 16 bits that follow the code plus 16 random bits reach 2^16, and r, if it is not zero, at least to the smallest
+ * code.  The random bits are the halves (high: m, low: r) of x = mix(i ^ t * 0x9E3779B9) for element i of its tensor,
+ * mix: x ^= x >> 16, x *= 0x7FEB352D, x ^= x >> 15, x *= 0x846CA68B, x ^= x >> 16 in 32 bits.  (To nearest, a state that
+ * changes by a thousandth a step would stand still, and one that draws from its own discarded bits does where there is
+ * no gradient: the same code times the same constant leaves the same bits.)
+ * An element whose scaled gradient is not finite keeps its weight, m and v, and raises NITI_DEV_NONFINITE. */
+#define NITI_STATE_BLOCK 256
+typedef struct niti_adamw_tensor {
+  float *p;
+  const void *g;             /* of type g_type */
+  void *m, *v;
+  int8_t *s_m, *s_v;         /* 8-bit states only */
+  int8_t *w8;                /* may be NULL */
+  const int32_t *s_w;
+  int64_t n;
+  float weight_decay;
+  int32_t g_type;            /* NITI_F32, NITI_BF16 or NITI_F16 */
+} niti_adamw_tensor;
+int niti_adamw(niti_ctx *ctx, void *stream, const niti_adamw_tensor *tensors, int n, int state_bits, const int32_t *step,
+               double lr, double beta1, double beta2, double eps, const float *grad_scale);
 
 #ifdef __cplusplus
 }

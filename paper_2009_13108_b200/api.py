@@ -17,6 +17,11 @@ OK, ERR_ARG, ERR_SHAPE, ERR_WORKSPACE, ERR_RANGE, ERR_CUDA, ERR_DEVICE = range(7
 ROUND_PSR, ROUND_NEAREST = 0, 1
 OP_LINEAR_FWD, OP_LINEAR_BWD, OP_CONV_FWD, OP_CONV_DGRAD, OP_CONV_WGRAD, OP_INT_XENT = range(6)
 OP_LINEAR_BWD_UPDATE, OP_CONV_WGRAD_UPDATE = 6, 7
+OP_RMSNORM_FWD, OP_RMSNORM_BWD, OP_QUANTIZE = 8, 9, 10
+F32, BF16, F16 = 0, 1, 2
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+I8, E4M3 = 0, 1
+STATE_BLOCK = 256
 REDUCE_MAX_U32, REDUCE_MAX_U64, REDUCE_SUM_I32, REDUCE_SCATTER_SUM_I32, ALLGATHER_I8 = 0, 1, 2, 3, 4
 _REDUCE_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int)
 
@@ -29,6 +34,7 @@ EXPORTS = [
     "niti_conv_wgrad_update", "niti_linear_bwd_update", "niti_int_xent", "niti_int_xent_noalloc", "niti_int_sgd_update",
     "niti_copy_tensors", "niti_relu_fwd",
     "niti_relu_bwd", "niti_maxpool2_fwd", "niti_maxpool2_bwd", "niti_maxpool2_fwd_idx", "niti_maxpool2_bwd_idx",
+    "niti_rmsnorm_fwd", "niti_rmsnorm_bwd", "niti_quantize", "niti_dequantize", "niti_adamw",
 ]
 
 
@@ -105,7 +111,30 @@ def load_library():
     lib.niti_maxpool2_bwd.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32]
     lib.niti_maxpool2_fwd_idx.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32]
     lib.niti_maxpool2_bwd_idx.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32]
+    f32, f64 = C.c_float, C.c_double
+    lib.niti_rmsnorm_fwd.argtypes = [vp] * 9 + [i32, i32, i32, i32, f32, i32, vp, sz]
+    lib.niti_rmsnorm_bwd.argtypes = [vp] * 9 + [i32, i32, i32, vp, sz]
+    lib.niti_quantize.argtypes = [vp] * 5 + [i32, i32, i32, i32, i32, vp, sz]
+    lib.niti_dequantize.argtypes = [vp] * 5 + [i32, i32, i32, i64, i64]
+    lib.niti_adamw.argtypes = [vp, vp, C.POINTER(_AdamwTensor), i32, i32, vp, f64, f64, f64, f64, vp]
     return lib
+
+
+class _AdamwTensor(C.Structure):
+    """niti_adamw_tensor"""
+    _fields_ = [("p", C.c_void_p), ("g", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p), ("s_m", C.c_void_p),
+                ("s_v", C.c_void_p), ("w8", C.c_void_p), ("s_w", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("g_type", C.c_int32)]
+
+
+class AdamwTensors:
+    """The tensor list of ``Niti.adamw``: built once by ``Niti.adamw_tensors``, it holds the tensors it points to."""
+
+    def __init__(self, array, state_bits, tensors):
+        self.array, self.state_bits, self.tensors = array, state_bits, tensors
+
+    def __len__(self):
+        return len(self.array)
 
 
 def _ptr(t):
@@ -514,6 +543,144 @@ class Niti:
         self._ck(self.lib.niti_maxpool2_bwd(self.h, self._stream(), _ptr(x), _ptr(e_out),
                                             _ptr(e_in), B, H, W, Cc, int(relu)))
         return e_in
+
+    # ---- float tensors at the boundary of the format ----
+    def _tensor(self, t, name, shape=None, dtype=None):
+        """An operand the library may be given the pointer of, or NitiError."""
+        if t.get_device() != self.device.index or not t.is_contiguous():
+            raise NitiError(ERR_ARG, "%s: a contiguous tensor on %s is needed" % (name, self.device))
+        if dtype is not None and t.dtype != dtype:
+            raise NitiError(ERR_ARG, "%s: %s needed, got %s" % (name, dtype, t.dtype))
+        if shape is not None and t.shape != shape:
+            raise NitiError(ERR_ARG, "%s: shape %s needed, got %s" % (name, tuple(shape), tuple(t.shape)))
+        return t
+
+    def _float(self, t, name):
+        """(type id) of an activation tensor."""
+        self._tensor(t, name)
+        if t.dtype not in _TYPES or t.dim() != 2:
+            raise NitiError(ERR_ARG, "%s: a matrix of float32, bfloat16 or float16 is needed" % name)
+        return _TYPES[t.dtype]
+
+    def _out(self, t, name, shape, dtype):
+        """A caller's output after its check, or a new one."""
+        if t is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        return self._tensor(t, name, shape, dtype)
+
+    def rmsnorm_fwd(self, x, gain, residual=None, h=None, y=None, s_y=None, rstd=None, rows=True, eps=1e-6,
+                    round_mode=ROUND_NEAREST):
+        """niti_rmsnorm_fwd: (payload, exponents [M] or with ``rows=False`` [1], h = x + residual, 1 / rms).  Without a
+        residual h is x."""
+        type_id = self._float(x, "x")
+        M, Cc = x.shape
+        self._tensor(gain, "gain", (Cc,), torch.float32)
+        if residual is None:
+            if h is not None:
+                raise NitiError(ERR_ARG, "h: written only with a residual")
+        else:
+            self._tensor(residual, "residual", x.shape, x.dtype)
+            h = self._out(h, "h", x.shape, x.dtype)
+        y = self._out(y, "y", x.shape, torch.int8)
+        s_y = self._out(s_y, "s_y", (M if rows else 1,), torch.int32)
+        rstd = self._out(rstd, "rstd", (M,), torch.float32)
+        ws, wsb = self._ws_for(OP_RMSNORM_FWD, M, Cc)
+        self._ck(self.lib.niti_rmsnorm_fwd(self.h, self._stream(), _ptr(x), _ptr(residual), _ptr(gain), _ptr(h), _ptr(y),
+                                           _ptr(s_y), _ptr(rstd), type_id, M, Cc, int(rows), eps, round_mode, ws, wsb))
+        return y, s_y, (x if h is None else h), rstd
+
+    def rmsnorm_bwd(self, dy, h, gain, rstd, dh=None, dx=None, dgain=None, need_dgain=True):
+        """niti_rmsnorm_bwd: (dx, dgain); ``dh`` is the gradient that reaches h past the norm."""
+        type_id = self._float(dy, "dy")
+        M, Cc = dy.shape
+        self._tensor(h, "h", dy.shape, dy.dtype)
+        self._tensor(gain, "gain", (Cc,), torch.float32)
+        self._tensor(rstd, "rstd", (M,), torch.float32)
+        if dh is not None:
+            self._tensor(dh, "dh", dy.shape, dy.dtype)
+        dx = self._out(dx, "dx", dy.shape, dy.dtype)
+        dgain = self._out(dgain, "dgain", (Cc,), torch.float32) if need_dgain else None
+        ws, wsb = self._ws_for(OP_RMSNORM_BWD, M, Cc)
+        self._ck(self.lib.niti_rmsnorm_bwd(self.h, self._stream(), _ptr(dy), _ptr(h), _ptr(gain), _ptr(rstd), _ptr(dh),
+                                           _ptr(dx), _ptr(dgain), type_id, M, Cc, ws, wsb))
+        return dx, dgain
+
+    def quantize(self, x, q=None, s=None, rows=True, round_mode=ROUND_NEAREST):
+        """niti_quantize: (payload, exponents) of a float matrix."""
+        type_id = self._float(x, "x")
+        M, Cc = x.shape
+        q = self._out(q, "q", x.shape, torch.int8)
+        s = self._out(s, "s", (M if rows else 1,), torch.int32)
+        ws, wsb = self._ws_for(OP_QUANTIZE, M, Cc)
+        self._ck(self.lib.niti_quantize(self.h, self._stream(), _ptr(x), _ptr(q), _ptr(s), type_id, M, Cc, int(rows),
+                                        round_mode, ws, wsb))
+        return q, s
+
+    def dequantize(self, q, s, dtype=torch.float32, out=None, block=None):
+        """niti_dequantize: the values of int8 payloads, or of the uint8 codes of an 8-bit state, with one exponent in all,
+        one per row of ``q``, or one for every ``block`` elements (the last block may be short)."""
+        self._tensor(q, "q")
+        self._tensor(s, "s")
+        n, per = q.numel(), block
+        if per is None and s.numel() != 1:
+            per = q.shape[-1]
+        if q.dtype not in (torch.int8, torch.uint8) or s.dtype not in (torch.int32, torch.int8) or dtype not in _TYPES:
+            raise NitiError(ERR_ARG, "dequantize: int8 or uint8 elements, int32 or int8 exponents, a float result")
+        if s.numel() != (1 if per is None else -(-n // per) if per > 0 else -1) and n:
+            raise NitiError(ERR_ARG, "dequantize: %d exponents for %d elements, %s each" % (s.numel(), n, per or "all"))
+        out = self._out(out, "out", q.shape, dtype)
+        self._ck(self.lib.niti_dequantize(self.h, self._stream(), _ptr(q), _ptr(s), _ptr(out),
+                                          I8 if q.dtype == torch.int8 else E4M3, s.element_size(), _TYPES[dtype], n, per or 0))
+        return out
+
+    def adamw_state(self, p, bits=8):
+        """Fresh states of a weight tensor for ``adamw_tensors``: (m, v, s_m, s_v), the exponents None with 32 bits."""
+        if bits == 32:
+            return torch.zeros_like(p), torch.zeros_like(p), None, None
+        blocks = -(-p.numel() // STATE_BLOCK)
+        return (torch.zeros_like(p, dtype=torch.uint8), torch.zeros_like(p, dtype=torch.uint8),
+                torch.zeros(blocks, dtype=torch.int8, device=p.device), torch.zeros(blocks, dtype=torch.int8, device=p.device))
+
+    def adamw_tensors(self, params, grads, m, v, s_m=None, s_v=None, w8=None, s_w=None, weight_decay=0.0):
+        """The list that ``adamw`` works on: float32 weights, gradients (float32, bfloat16 or float16), states (float32, or
+        uint8 codes with int8 exponents per 256 elements), and optionally int8 weights with their exponents (device int32
+        scalars).  ``weight_decay``: one number, or one per tensor.  The list keeps the tensors alive; their storage is
+        read and written by every ``adamw`` call on it."""
+        n = len(params)
+        eight = s_m is not None
+        none = [None] * n
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        lists = [list(x) if x is not None else none for x in (grads, m, v, s_m, s_v, w8, s_w)]
+        if any(len(x) != n for x in lists + [decay]) or (s_m is None) != (s_v is None) or (w8 is None) != (s_w is None):
+            raise NitiError(ERR_ARG, "adamw_tensors: lists of one length; s_m with s_v, w8 with s_w")
+        array = (_AdamwTensor * n)()
+        state = torch.uint8 if eight else torch.float32
+        for i, (p, g, mi, vi, sm, sv, w, sw) in enumerate(zip(params, *lists)):
+            name = "tensor %d: " % i
+            self._tensor(p, name + "p", None, torch.float32)
+            self._tensor(g, name + "g", p.shape)
+            if g.dtype not in _TYPES:
+                raise NitiError(ERR_ARG, name + "a gradient of float32, bfloat16 or float16 is needed")
+            self._tensor(mi, name + "m", p.shape, state)
+            self._tensor(vi, name + "v", p.shape, state)
+            if eight:
+                blocks = (-(-p.numel() // STATE_BLOCK),)
+                self._tensor(sm, name + "s_m", blocks, torch.int8)
+                self._tensor(sv, name + "s_v", blocks, torch.int8)
+            if w is not None:
+                self._tensor(w, name + "w8", p.shape, torch.int8)
+                self._tensor(sw, name + "s_w", None, torch.int32)
+            array[i] = _AdamwTensor(_ptr(p), _ptr(g), _ptr(mi), _ptr(vi), _ptr(sm), _ptr(sv), _ptr(w), _ptr(sw), p.numel(),
+                                    decay[i], _TYPES[g.dtype])
+        return AdamwTensors(array, 8 if eight else 32, [list(params)] + lists)
+
+    def adamw(self, tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
+        """niti_adamw on a list of ``adamw_tensors``; ``step``: device int32 scalar, the number of this step (from 1)."""
+        self._tensor(step, "step", None, torch.int32)
+        if grad_scale is not None:
+            self._tensor(grad_scale, "grad_scale", None, torch.float32)
+        self._ck(self.lib.niti_adamw(self.h, self._stream(), tensors.array, len(tensors), tensors.state_bits, _ptr(step), lr,
+                                     betas[0], betas[1], eps, _ptr(grad_scale)))
 
 
 def _device_view(ptr: int, nbytes: int, device):

@@ -2,6 +2,7 @@
 // accumulate -> bit-width -> shift-and-round sequence of Algorithm 1 for each layer op.
 #include "niti_common.cuh"
 
+size_t niti_norm_ws_bytes(int op, long long M, long long C);
 int niti_launch_im2col32(niti_ctx *ctx, cudaStream_t st, const int8_t *x, int8_t *xcol, int B, int H, int W,
                          int Ci, int R, int S, int pad, int stride, int Ho, int Wo);
 int niti_launch_widen(niti_ctx *ctx, cudaStream_t st, const int8_t *x, int8_t *xw, int rows, int W, int Ci, int Cp, int pad,
@@ -397,6 +398,11 @@ extern "C" size_t niti_workspace_bytes(int op, const int64_t *d, int nd) {
       if (nd != 2 || d[0] <= 0 || d[1] <= 0) return 0;
       // two 64-bit scalars per sample
       return NITI_WS_HEADER + round_up((size_t)d[0] * 16, 256);
+    case NITI_OP_RMSNORM_FWD:
+    case NITI_OP_RMSNORM_BWD:
+    case NITI_OP_QUANTIZE:
+      if (nd != 2 || d[0] < 0 || d[1] <= 0) return 0;
+      return niti_norm_ws_bytes(op, d[0], d[1]);
     default:
       return 0;
   }

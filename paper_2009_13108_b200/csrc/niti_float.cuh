@@ -1,0 +1,121 @@
+// Floating-point tensors at the boundary of the integer format: types, vector accesses, and the rounding of a float to an
+// int8 payload with a power-of-two exponent (value = payload * 2^s).
+#pragma once
+#include "niti_common.cuh"
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+template <int T> struct FloatOf;
+template <> struct FloatOf<NITI_F32> { typedef float type; };
+template <> struct FloatOf<NITI_BF16> { typedef __nv_bfloat16 type; };
+template <> struct FloatOf<NITI_F16> { typedef __half type; };
+static inline int niti_type_size(int type) { return type == NITI_F32 ? 4 : 2; }
+static inline bool niti_type_ok(int type) { return type == NITI_F32 || type == NITI_BF16 || type == NITI_F16; }
+
+// VEC consecutive elements as the words that one access moves: 16 bytes, or a single element.
+template <int T, int VEC>
+struct Pack {
+  static constexpr int BYTES = VEC * (int)sizeof(typename FloatOf<T>::type);
+  static_assert(BYTES == 16 || VEC == 1, "16-byte vectors or single elements");
+  static constexpr int WORDS = (BYTES + 3) / 4;
+  unsigned w[WORDS];
+
+  // (streaming: every element of these tensors is read once per launch)
+  __device__ __forceinline__ void load(const void *p, long long i) {
+    const char *q = reinterpret_cast<const char *>(p) + i * (long long)sizeof(typename FloatOf<T>::type);
+    if constexpr (BYTES == 16) {
+      const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(q));
+      w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    } else if constexpr (BYTES == 4) {
+      w[0] = *reinterpret_cast<const unsigned *>(q);
+    } else {
+      w[0] = *reinterpret_cast<const unsigned short *>(q);
+    }
+  }
+  __device__ __forceinline__ void store(void *p, long long i) const {
+    char *q = reinterpret_cast<char *>(p) + i * (long long)sizeof(typename FloatOf<T>::type);
+    if constexpr (BYTES == 16) *reinterpret_cast<uint4 *>(q) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if constexpr (BYTES == 4) *reinterpret_cast<unsigned *>(q) = w[0];
+    else *reinterpret_cast<unsigned short *>(q) = (unsigned short)w[0];
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) w[i] = 0u;
+  }
+  __device__ __forceinline__ float get(int j) const {
+    if constexpr (T == NITI_F32) return __uint_as_float(w[j]);
+    else if constexpr (T == NITI_BF16) return __uint_as_float((j & 1) ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+    else return __half2float(__ushort_as_half((unsigned short)((j & 1) ? w[j >> 1] >> 16 : w[j >> 1])));
+  }
+  // rounded to the type (to nearest even)
+  __device__ __forceinline__ void set(const float (&v)[VEC]) {
+    if constexpr (T == NITI_F32) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) w[j] = __float_as_uint(v[j]);
+    } else if constexpr (VEC == 1) {
+      if constexpr (T == NITI_BF16) w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+      else w[0] = __half_as_ushort(__float2half_rn(v[0]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < WORDS; ++j) {
+        if constexpr (T == NITI_BF16) {
+          const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+          w[j] = *reinterpret_cast<const unsigned *>(&p);
+        } else {
+          const __half2 p = __floats2half2_rn(v[2 * j], v[2 * j + 1]);
+          w[j] = *reinterpret_cast<const unsigned *>(&p);
+        }
+      }
+    }
+  }
+};
+
+// ---- rounding to payloads -------------------------------------------------------------------
+// Exponent of a tensor (or row) whose largest magnitude has these bits: the one that leaves seven integer bits, so that
+// payload magnitudes reach 64 .. 127 (the effective bit-width rule of Section 3.2 on floats).  Not below NITI_EXP_LOWEST
+// (2^-s stays a normal float); 0 for a tensor of zeros; that of the largest finite magnitude where one is not finite.
+#define NITI_EXP_LOWEST (-100)
+__device__ __forceinline__ int niti_exponent_of(unsigned max_bits, int integer_bits = 7) {
+  if (max_bits == 0u) return 0;
+  const int e = (int)(max_bits >> 23);
+  const int s = (e > 254 ? 254 : e) - 126 - integer_bits;
+  return s < NITI_EXP_LOWEST ? NITI_EXP_LOWEST : s;
+}
+// 2^e for e in [-126, 127]
+__device__ __forceinline__ float niti_pow2(int e) { return __int_as_float((e + 127) << 23); }
+
+// Magnitude u in units of the result to a whole number, at most 127.  Pseudo-stochastic: the 16 fraction bits are split
+// into halves, rounded up where the top half is larger than the bottom half (Algorithm 3 with bp = 16; the sum carries
+// into bit 16 exactly then).  To nearest: half up, as everywhere in the library.  (Conversions saturate, and turn NaN
+// into 0.)
+__device__ __forceinline__ int niti_round_units(float u, int round_mode) {
+  unsigned q;
+  if (round_mode == NITI_ROUND_PSR) {
+    const unsigned v = __float2uint_rz(u * 65536.0f);
+    q = v >= (127u << 16) ? 127u : (v + ((~v & 255u) << 8)) >> 16;
+  } else {
+    q = __float2uint_rz(u + 0.5f);
+  }
+  return (int)(q > 127u ? 127u : q);
+}
+// scale = 2^-s (times whatever else scales the tensor)
+__device__ __forceinline__ int niti_payload(float x, float scale, int round_mode) {
+  const int q = niti_round_units(fabsf(x) * scale, round_mode);
+  return x < 0.0f ? -q : q;
+}
+
+// VEC payload bytes at p + i
+template <int VEC>
+__device__ __forceinline__ void niti_store_payload(int8_t *p, long long i, const int (&q)[VEC]) {
+  if constexpr (VEC == 1) {
+    p[i] = (int8_t)q[0];
+  } else {
+    unsigned w[VEC / 4];
+#pragma unroll
+    for (int j = 0; j < VEC / 4; ++j)
+      w[j] = (unsigned)(q[4 * j] & 255) | (unsigned)(q[4 * j + 1] & 255) << 8 | (unsigned)(q[4 * j + 2] & 255) << 16 |
+             (unsigned)q[4 * j + 3] << 24;
+    if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(p + i) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<unsigned *>(p + i) = w[0];
+  }
+}

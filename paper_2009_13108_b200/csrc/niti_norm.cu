@@ -1,0 +1,656 @@
+// Root-mean-square norm with the residual's addition and an int8 result, its backward pass, and the conversions between
+// float tensors and payloads.  All of these are bound by HBM: a row is read once and stays in registers while its sums are
+// taken.
+#include "niti_div.h"
+#include "niti_float.cuh"
+#include <type_traits>
+
+namespace {
+
+constexpr int ROW_THREADS = 256;      // threads of a block where a row takes fewer
+constexpr int ROW_MOST = 512;         // and at most (a thread keeps up to 32 values of a row and as many gains)
+constexpr unsigned INF_BITS = 0x7f800000u;
+
+struct RowShape {
+  int M, C;
+  int tpr;                            // threads of a row (a multiple of 32)
+  int rpb;                            // rows of a block
+};
+
+// Sum of `ss` and maximum of `am` over the threads of a row, in a fixed order.  buf: per warp of the block.  One barrier a
+// row: consecutive rows use the two halves of `buf` in turn.
+__device__ __forceinline__ void row_reduce(float &ss, unsigned &am, int tpr, int warp, int lane, float2 (*buf)[32], int turn) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  am = __reduce_max_sync(0xffffffffu, am);
+  if (tpr == 32) return;
+  const int wpr = tpr >> 5, first = warp / wpr * wpr;
+  if (lane == 0) buf[turn][warp] = make_float2(ss, __uint_as_float(am));
+  __syncthreads();
+  const float2 v = lane < wpr ? buf[turn][first + lane] : make_float2(0.0f, 0.0f);
+  ss = v.x;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+  am = __reduce_max_sync(0xffffffffu, __float_as_uint(v.y));
+}
+
+// y = h r gain with h = x + residual, r = 1 / sqrt(mean(h^2) + eps); without NORM y = x.  A thread holds NV vectors of its
+// row, and the next row's are on their way while this one's sums are taken.  The maximum that fixes the exponent is taken
+// of |h gain| beside the sum of squares, since r only scales it: one reduction a row.
+// SHARED: only h, r and the maximum over the tensor; norm_round_kernel follows.
+template <int T, int VEC, int NV, bool NORM, bool SHARED>
+__global__ void __launch_bounds__(ROW_MOST)
+norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int8_t *y, int32_t *s_y, float *rstd,
+                 WsHeader *hdr, WsHeader *next, uint32_t *status, RowShape sh, float eps, int round_mode) {
+  __shared__ float2 buf[2][32];
+  niti_enter(x, res, gain);
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const int grp = (int)threadIdx.x / sh.tpr, t = (int)threadIdx.x - grp * sh.tpr;
+  if (next && blockIdx.x == 0 && warp == 0) niti_zero_header(next, lane);
+  float g[NV][VEC];
+  Pack<T, VEC> px[NV], pr[NV];
+  bool in[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * sh.tpr + t) * VEC;
+    in[v] = c < sh.C;
+    px[v].zero(); pr[v].zero();
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) g[v][j] = NORM && in[v] ? gain[c + j] : 1.0f;
+  }
+  const int step = (int)gridDim.x * sh.rpb;
+  auto fetch = [&](int row) {
+    const long long at = (long long)row * sh.C + t * VEC;
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (in[v] && row < sh.M) {
+        px[v].load(x, at + (long long)v * sh.tpr * VEC);
+        if (NORM && res) pr[v].load(res, at + (long long)v * sh.tpr * VEC);
+      }
+  };
+  int row = (int)blockIdx.x * sh.rpb + grp;
+  fetch(row);
+  unsigned most = 0;
+  for (int turn = 0, base = (int)blockIdx.x * sh.rpb; base < sh.M; base += step, row += step, turn ^= 1) {
+    const bool rok = row < sh.M;
+    const long long at = (long long)row * sh.C + t * VEC;
+    float hv[NV][VEC];
+    float ss = 0.0f;
+    unsigned am = 0;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) hv[v][j] = px[v].get(j);
+      if (NORM && res) {
+        Pack<T, VEC> ph;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) hv[v][j] += pr[v].get(j);
+        ph.set(hv[v]);
+        if (in[v] && rok) ph.store(h, at + (long long)v * sh.tpr * VEC);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) hv[v][j] = ph.get(j);         // (the norm is that of the stored row)
+      }
+    }
+    fetch(row + step < sh.M ? row + step : sh.M);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        if (NORM) ss = fmaf(hv[v][j], hv[v][j], ss);
+        hv[v][j] *= g[v][j];
+        if (in[v]) am = max(am, __float_as_uint(hv[v][j]) & 0x7fffffffu);
+      }
+    row_reduce(ss, am, sh.tpr, warp, lane, buf, turn);
+    const float r = NORM ? rsqrtf(ss / (float)sh.C + eps) : 1.0f;
+    // (r is 0 or NaN where the squares left the float range, and then nothing of the row means anything)
+    const unsigned top = am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
+    if (t == 0 && rok) {
+      if (top >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
+      if (NORM && rstd) rstd[row] = r;
+    }
+    if (SHARED) {
+      if (rok) most = max(most, top);
+      continue;
+    }
+    const int s = niti_exponent_of(top);
+    const float scale = r * niti_pow2(-s);
+    if (t == 0 && rok) s_y[row] = s;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      int q[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) q[j] = niti_payload(hv[v][j], scale, round_mode);
+      if (in[v] && rok) niti_store_payload<VEC>(y, at + (long long)v * sh.tpr * VEC, q);
+    }
+  }
+  if (SHARED) {
+    most = __reduce_max_sync(0xffffffffu, most);
+    if (lane == 0 && most) atomicMax(&hdr->maxabs32, most);
+  }
+}
+
+// Payload of a whole tensor with the exponent of its maximum, from h (or x) and r.  The rows that norm_rows_kernel read
+// last come first: they are still in L2.
+template <int T, int VEC, bool NORM>
+__global__ void __launch_bounds__(ROW_THREADS)
+norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y, int32_t *s_y, const WsHeader *hdr, int M, int C,
+                  int parts, int round_mode) {
+  niti_enter(h, gain, rstd, hdr);
+  const int s = niti_exponent_of(hdr->maxabs32);
+  const float p2 = niti_pow2(-s);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *s_y = s;
+  const long long items = (long long)M * parts;
+  for (long long it = (long long)gridDim.x - 1 - blockIdx.x; it < items; it += gridDim.x) {
+    const int row = M - 1 - (int)(it / parts), part = (int)(it % parts);
+    const int c = (part * ROW_THREADS + (int)threadIdx.x) * VEC;
+    if (c >= C) continue;
+    const float scale = NORM ? rstd[row] * p2 : p2;
+    Pack<T, VEC> p;
+    p.load(h, (long long)row * C + c);
+    int q[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) q[j] = niti_payload(NORM ? p.get(j) * gain[c + j] : p.get(j), scale, round_mode);
+    niti_store_payload<VEC>(y, (long long)row * C + c, q);
+  }
+}
+
+// Rows that are longer than a block's registers: the row is read again (from L2) for the rounding.
+template <int T, bool NORM, bool SHARED>
+__global__ void __launch_bounds__(1024)
+norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int8_t *y, int32_t *s_y, float *rstd,
+                 WsHeader *hdr, WsHeader *next, uint32_t *status, int M, int C, float eps, int round_mode) {
+  __shared__ float2 buf[2][32];
+  niti_enter(x, res, gain);
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  if (next && blockIdx.x == 0 && warp == 0) niti_zero_header(next, lane);
+  unsigned most = 0;
+  int turn = 0;
+  for (int row = (int)blockIdx.x; row < M; row += (int)gridDim.x, turn ^= 1) {
+    const long long at = (long long)row * C;
+    float ss = 0.0f;
+    unsigned am = 0;
+    for (int c = (int)threadIdx.x; c < C; c += 1024) {
+      Pack<T, 1> p;
+      p.load(x, at + c);
+      float v = p.get(0);
+      if (NORM && res) {
+        Pack<T, 1> pr;
+        pr.load(res, at + c);
+        const float sum[1] = {v + pr.get(0)};
+        p.set(sum);
+        p.store(h, at + c);
+        v = p.get(0);
+      }
+      if (NORM) ss = fmaf(v, v, ss);
+      am = max(am, __float_as_uint(NORM ? v * gain[c] : v) & 0x7fffffffu);
+    }
+    row_reduce(ss, am, 1024, warp, lane, buf, turn);
+    const float r = NORM ? rsqrtf(ss / (float)C + eps) : 1.0f;
+    const unsigned top = am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
+    if (threadIdx.x == 0) {
+      if (top >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
+      if (NORM && rstd) rstd[row] = r;
+    }
+    if (SHARED) {
+      most = max(most, top);
+      continue;
+    }
+    const int s = niti_exponent_of(top);
+    const float scale = r * niti_pow2(-s);
+    if (threadIdx.x == 0) s_y[row] = s;
+    const void *src = NORM && res ? h : x;            // (each thread reads what it has written itself)
+    for (int c = (int)threadIdx.x; c < C; c += 1024) {
+      Pack<T, 1> p;
+      p.load(src, at + c);
+      y[at + c] = (int8_t)niti_payload(NORM ? p.get(0) * gain[c] : p.get(0), scale, round_mode);
+    }
+  }
+  if (SHARED && threadIdx.x == 0 && most) atomicMax(&hdr->maxabs32, most);
+}
+
+// Backward: with G = gain dy and c = sum_c(G h) r^3 / C:  dx = dh + r G - c h;  dgain = sum over the rows of dy h r.  The
+// columns of a thread are the same in every row, so the gain's gradient stays in its registers; each block leaves its sums
+// in `part` and gain_sum_kernel adds them up in a fixed order.
+template <int T, int VEC, int NV>
+__global__ void __launch_bounds__(ROW_MOST)
+norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, float *part,
+                RowShape sh) {
+  __shared__ float2 buf[2][32];
+  niti_enter(dy, h, gain, rstd, dh);
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  const int grp = (int)threadIdx.x / sh.tpr, t = (int)threadIdx.x - grp * sh.tpr;
+  float g[NV][VEC], dg[NV][VEC];
+  Pack<T, VEC> py[NV], ph[NV], pd[NV];
+  bool in[NV];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int c = (v * sh.tpr + t) * VEC;
+    in[v] = c < sh.C;
+    py[v].zero(); ph[v].zero(); pd[v].zero();
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      g[v][j] = in[v] ? gain[c + j] : 0.0f;
+      dg[v][j] = 0.0f;
+    }
+  }
+  const int step = (int)gridDim.x * sh.rpb;
+  float r_next = 0.0f;
+  auto fetch = [&](int row) {
+    if (row >= sh.M) return;
+    const long long at = (long long)row * sh.C + t * VEC;
+    r_next = rstd[row];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+      if (in[v]) {
+        py[v].load(dy, at + (long long)v * sh.tpr * VEC);
+        ph[v].load(h, at + (long long)v * sh.tpr * VEC);
+        if (dh) pd[v].load(dh, at + (long long)v * sh.tpr * VEC);
+      }
+  };
+  int row = (int)blockIdx.x * sh.rpb + grp;
+  fetch(row);
+  for (int turn = 0, base = (int)blockIdx.x * sh.rpb; base < sh.M; base += step, row += step, turn ^= 1) {
+    const bool rok = row < sh.M;
+    const float r = r_next;
+    Pack<T, VEC> qy[NV], qh[NV], qd[NV];
+    float dot = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      qy[v] = py[v]; qh[v] = ph[v]; qd[v] = pd[v];
+    }
+    fetch(row + step);
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float y = qy[v].get(j), hh = qh[v].get(j);
+        dot = fmaf(y * g[v][j], hh, dot);
+        if (rok) dg[v][j] = fmaf(y, hh * r, dg[v][j]);
+      }
+    unsigned none = 0;
+    row_reduce(dot, none, sh.tpr, warp, lane, buf, turn);
+    const float c = dot / (float)sh.C * (r * r * r);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      float d[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) d[j] = qd[v].get(j) + (r * (qy[v].get(j) * g[v][j]) - c * qh[v].get(j));
+      Pack<T, VEC> o;
+      o.set(d);
+      if (in[v] && rok) o.store(dx, (long long)row * sh.C + (v * sh.tpr + t) * VEC);
+    }
+  }
+  if (!part) return;
+  extern __shared__ float sums[];                    // (several rows a block: theirs first)
+  float *mine = sh.rpb > 1 ? sums + grp * sh.C : part + (long long)blockIdx.x * sh.C;
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+      if (in[v]) mine[(v * sh.tpr + t) * VEC + j] = dg[v][j];
+  if (sh.rpb == 1) return;
+  __syncthreads();
+  for (int c = (int)threadIdx.x; c < sh.C; c += (int)blockDim.x) {
+    float sum = sums[c];
+    for (int k = 1; k < sh.rpb; ++k) sum += sums[k * sh.C + c];
+    part[(long long)blockIdx.x * sh.C + c] = sum;
+  }
+}
+
+// Backward of rows longer than a block's registers: one block per row reads it twice and leaves dy h r to be summed by
+// columns in a second pass (norm_wide_gain_kernel).
+template <int T>
+__global__ void __launch_bounds__(1024)
+norm_bwd_wide_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, int M, int C) {
+  __shared__ float2 buf[2][32];
+  niti_enter(dy, h, gain, rstd, dh);
+  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+  int turn = 0;
+  for (int row = (int)blockIdx.x; row < M; row += (int)gridDim.x, turn ^= 1) {
+    const long long at = (long long)row * C;
+    const float r = rstd[row];
+    float dot = 0.0f;
+    unsigned none = 0;
+    Pack<T, 1> a, b, d;
+    d.zero();
+    for (int c = (int)threadIdx.x; c < C; c += 1024) {
+      a.load(dy, at + c);
+      b.load(h, at + c);
+      dot = fmaf(a.get(0) * gain[c], b.get(0), dot);
+    }
+    row_reduce(dot, none, 1024, warp, lane, buf, turn);
+    const float k = dot / (float)C * (r * r * r);
+    for (int c = (int)threadIdx.x; c < C; c += 1024) {
+      a.load(dy, at + c);
+      b.load(h, at + c);
+      if (dh) d.load(dh, at + c);
+      const float o[1] = {d.get(0) + (r * (a.get(0) * gain[c]) - k * b.get(0))};
+      Pack<T, 1> po;
+      po.set(o);
+      po.store(dx, at + c);
+    }
+  }
+}
+// Column sums of dy h r over a share of the rows (blockIdx.y), a thread per column; in front of norm_bwd_wide_kernel, which
+// may write dx over dy.
+template <int T>
+__global__ void __launch_bounds__(256)
+norm_wide_gain_kernel(const void *dy, const void *h, const float *rstd, float *part, int M, int C) {
+  niti_enter(dy, h, rstd);
+  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+  if (c >= C) return;
+  float sum = 0.0f;
+  for (int row = (int)blockIdx.y; row < M; row += (int)gridDim.y) {
+    Pack<T, 1> a, b;
+    a.load(dy, (long long)row * C + c);
+    b.load(h, (long long)row * C + c);
+    sum = fmaf(a.get(0), b.get(0) * rstd[row], sum);
+  }
+  part[(long long)blockIdx.y * C + c] = sum;
+}
+
+// dst[c] = sum over the rows of part[n][C]: 32 columns a block, eight threads a column.
+__global__ void __launch_bounds__(256)
+gain_sum_kernel(const float *part, float *dst, int n, int C) {
+  __shared__ float buf[8][33];
+  niti_enter(part);
+  const int tx = (int)threadIdx.x & 31, ty = (int)threadIdx.x >> 5;
+  const int c = (int)blockIdx.x * 32 + tx;
+  float sum = 0.0f;
+  if (c < C)
+    for (int i = ty; i < n; i += 8) sum += part[(long long)i * C + c];
+  buf[ty][tx] = sum;
+  __syncthreads();
+  if (ty == 0 && c < C) {
+#pragma unroll
+    for (int k = 1; k < 8; ++k) sum += buf[k][tx];
+    dst[c] = sum;
+  }
+}
+
+// values = payload * 2^s, or the value of an 8-bit code times 2^s; one exponent for every `per` elements.  16 elements a
+// thread where WIDE.
+template <int T, bool E4M3, typename S, bool WIDE>
+__global__ void __launch_bounds__(256)
+dequantize_kernel(const uint8_t *q, const S *s, void *out, long long n, Div d_per, long long per) {
+  niti_enter(q, s);
+  constexpr int VEC = WIDE ? 16 : 1;
+  const long long items = n / VEC;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
+    const long long at = i * VEC;
+    // (WIDE: `per` counts vectors and items are below 2^31)
+    const int e = (int)s[per == 0 ? 0 : WIDE ? (long long)div_by((int)i, d_per) : at / per];
+    const float scale = e >= -126 && e <= 127 ? niti_pow2(e) : ldexpf(1.0f, e < -149 ? -149 : e > 128 ? 128 : e);
+    uint8_t b[VEC];
+    if constexpr (WIDE) {
+      const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(q) + i);
+      *reinterpret_cast<uint4 *>(b) = w;
+    } else {
+      b[0] = q[at];
+    }
+    float v[VEC];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      if (E4M3) {
+        // (the code's exponent and fraction, moved into place, are the value over 2^120; exact, the small ones too)
+        v[j] = __uint_as_float((unsigned)(b[j] & 127) << 20) * 1.329227995784916e+36f * scale;
+        if (b[j] & 128) v[j] = -v[j];
+      } else {
+        v[j] = (float)(int8_t)b[j] * scale;
+      }
+    }
+    if constexpr (WIDE) {
+      constexpr int PV = 16 / (int)sizeof(typename FloatOf<T>::type);
+#pragma unroll
+      for (int k = 0; k < 16 / PV; ++k) {
+        float part[PV];
+#pragma unroll
+        for (int j = 0; j < PV; ++j) part[j] = v[PV * k + j];
+        Pack<T, PV> p;
+        p.set(part);
+        p.store(out, at + PV * k);
+      }
+    } else {
+      Pack<T, 1> p;
+      p.set(v);
+      p.store(out, at);
+    }
+  }
+}
+
+inline bool misaligned(const void *a, uintptr_t bytes) { return ((uintptr_t)a & (bytes - 1)) != 0; }
+
+// How a row of C elements is dealt to threads: vectors of 16 bytes where rows and pointers allow them; as few vectors a
+// thread as keep a row within ROW_THREADS threads, then within ROW_MOST.
+struct RowPlan { int vec, nv; RowShape sh; };
+RowPlan plan_rows(int M, int C, int type, bool aligned, int nv_most) {
+  RowPlan p;
+  const int v16 = 16 / niti_type_size(type);
+  p.vec = aligned && C % v16 == 0 ? v16 : 1;
+  const int nvec = (C + p.vec - 1) / p.vec;
+  p.nv = 0;
+  p.sh.M = M; p.sh.C = C; p.sh.tpr = 0; p.sh.rpb = 1;
+  for (int limit = ROW_THREADS; limit <= ROW_MOST && !p.nv; limit *= 2)
+    for (int nv = 1; nv <= nv_most && !p.nv; nv *= 2)
+      if ((nvec + nv - 1) / nv <= limit) p.nv = nv;
+  if (!p.nv) return p;                               // (wide rows)
+  p.sh.tpr = ((nvec + p.nv - 1) / p.nv + 31) / 32 * 32;
+  p.sh.rpb = p.sh.tpr >= ROW_THREADS ? 1 : ROW_THREADS / p.sh.tpr;
+  return p;
+}
+
+template <typename F>
+int with_type(int type, F f) {
+  if (type == NITI_F32) return f(std::integral_constant<int, NITI_F32>{});
+  if (type == NITI_BF16) return f(std::integral_constant<int, NITI_BF16>{});
+  return f(std::integral_constant<int, NITI_F16>{});
+}
+
+unsigned row_blocks(const niti_ctx *ctx, const RowShape &sh, int threads, int per_sm_threads) {
+  const long long want = ((long long)sh.M + sh.rpb - 1) / sh.rpb;
+  const long long cap = (long long)ctx->sm_count * (per_sm_threads / threads > 0 ? per_sm_threads / threads : 1);
+  return (unsigned)(want < cap ? want : cap);
+}
+
+struct NormCall {
+  const void *x, *res;
+  const float *gain;
+  void *h;
+  int8_t *y;
+  int32_t *s_y;
+  float *rstd;
+  int type, M, C, rows, round_mode;
+  float eps;
+};
+
+template <bool NORM>
+int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
+  const uintptr_t all = (uintptr_t)c.x | (uintptr_t)c.res | (uintptr_t)c.h;
+  const bool aligned = (all & 15) == 0 && !misaligned(c.y, 8);
+  const RowPlan pl = plan_rows(c.M, c.C, c.type, aligned, 4);
+  WsHeader *hdr = nullptr, *next = nullptr;
+  float *rstd = c.rstd;
+  if (!c.rows) {
+    hdr = niti_take_header(ctx, st, ws);
+    const int rc = niti_clear(ctx, st, nullptr, 0, &next);
+    if (rc != NITI_OK) return rc;
+    if (NORM && !rstd) rstd = (float *)((char *)ws + NITI_WS_HEADER);
+  }
+  const int threads = pl.nv ? pl.sh.tpr * pl.sh.rpb : 1024;
+  const int rc = with_type(c.type, [&](auto t) -> int {
+    constexpr int T = decltype(t)::value;
+    constexpr int V16 = 16 / (int)sizeof(typename FloatOf<T>::type);
+    auto go = [&](auto shared) -> int {
+      constexpr bool SHARED = decltype(shared)::value;
+      auto rows = [&](auto vec, auto nv) -> int {
+        NITI_CUDA_TRY(ctx, niti_launch(st, row_blocks(ctx, pl.sh, threads, 768), threads, 0,
+                                       norm_rows_kernel<T, decltype(vec)::value, decltype(nv)::value, NORM, SHARED>, c.x, c.res, c.gain, c.h,
+                                       c.y, c.s_y, rstd, hdr, next, ctx->d_status, pl.sh, c.eps, c.round_mode));
+        return NITI_OK;
+      };
+      auto pick = [&](auto vec) -> int {
+        if (pl.nv == 1) return rows(vec, std::integral_constant<int, 1>{});
+        if (pl.nv == 2) return rows(vec, std::integral_constant<int, 2>{});
+        return rows(vec, std::integral_constant<int, 4>{});
+      };
+      if (!pl.nv) {
+        NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(c.M < 2 * ctx->sm_count ? c.M : 2 * ctx->sm_count), 1024, 0,
+                                       norm_wide_kernel<T, NORM, SHARED>, c.x, c.res, c.gain, c.h, c.y, c.s_y, rstd, hdr, next, ctx->d_status,
+                                       c.M, c.C, c.eps, c.round_mode));
+        return NITI_OK;
+      }
+      return pl.vec == 1 ? pick(std::integral_constant<int, 1>{}) : pick(std::integral_constant<int, V16>{});
+    };
+    int r = c.rows ? go(std::false_type{}) : go(std::true_type{});
+    ctx->launches++;
+    if (r != NITI_OK || c.rows) return r;
+    niti_header_passed_on(ctx, next);
+    const void *src = NORM && c.res ? c.h : c.x;
+    auto second = [&](auto vec) -> int {
+      constexpr int VEC = decltype(vec)::value;
+      const int parts = (c.C + ROW_THREADS * VEC - 1) / (ROW_THREADS * VEC);
+      const long long items = (long long)c.M * parts, cap = 8LL * ctx->sm_count;
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(items < cap ? items : cap), ROW_THREADS, 0, norm_round_kernel<T, VEC, NORM>, src,
+                                     c.gain, (const float *)rstd, c.y, c.s_y, (const WsHeader *)hdr, c.M, c.C, parts, c.round_mode));
+      return NITI_OK;
+    };
+    r = aligned && c.C % V16 == 0 ? second(std::integral_constant<int, V16>{}) : second(std::integral_constant<int, 1>{});
+    ctx->launches++;
+    return r;
+  });
+  return rc;
+}
+
+// Blocks of norm_bwd_kernel, whose gain sums the workspace has to hold: at most this many rows of C floats.
+constexpr int BWD_PARTS = 320;
+
+}  // namespace
+
+size_t niti_norm_ws_bytes(int op, long long M, long long C) {
+  if (op == NITI_OP_RMSNORM_BWD) return NITI_WS_HEADER + ((size_t)BWD_PARTS * 4 * (size_t)C + 255) / 256 * 256;
+  return NITI_WS_HEADER + ((size_t)M * 4 + 255) / 256 * 256;
+}
+
+static int norm_args(niti_ctx *ctx, const char *name, int type, int M, int C, void *ws, size_t ws_bytes, int op) {
+  if (!niti_type_ok(type) || M < 0 || C <= 0) {
+    snprintf(ctx->err, sizeof(ctx->err), "%s: bad argument (type, or a size that is not positive)", name);
+    return NITI_ERR_ARG;
+  }
+  if (M > (1 << 30)) return niti_fail(ctx, NITI_ERR_SHAPE, "more than 2^30 rows");            // (row counters have 32 bits)
+  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < niti_norm_ws_bytes(op, M, C))
+    return niti_fail(ctx, NITI_ERR_WORKSPACE, "workspace missing, misaligned or too small");
+  return NITI_OK;
+}
+
+extern "C" int niti_rmsnorm_fwd(niti_ctx *ctx, void *stream, const void *x, const void *residual, const float *gain, void *h, int8_t *y,
+                                int32_t *s_y, float *rstd, int type, int M, int C, int row_exponents, float eps, int round_mode, void *ws,
+                                size_t ws_bytes) {
+  if (!ctx) return NITI_ERR_ARG;
+  const int rc = norm_args(ctx, "niti_rmsnorm_fwd", type, M, C, ws, ws_bytes, NITI_OP_RMSNORM_FWD);
+  if (rc != NITI_OK || M == 0) return rc;
+  const uintptr_t es = (uintptr_t)niti_type_size(type);
+  if (!x || !gain || !y || !s_y || (residual && !h) || !(eps >= 0.0f) || (round_mode != NITI_ROUND_PSR && round_mode != NITI_ROUND_NEAREST) ||
+      (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)h) & (es - 1)) || (((uintptr_t)gain | (uintptr_t)s_y | (uintptr_t)rstd) & 3))
+    return niti_fail(ctx, NITI_ERR_ARG, "niti_rmsnorm_fwd: bad argument (a residual needs h; pointers are aligned to their type)");
+  const NormCall c = {x, residual, gain, residual ? h : nullptr, y, s_y, rstd, type, M, C, row_exponents, round_mode, eps};
+  return run_norm<true>(ctx, (cudaStream_t)stream, c, ws);
+}
+
+extern "C" int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t *q, int32_t *s, int type, int M, int C, int row_exponents,
+                             int round_mode, void *ws, size_t ws_bytes) {
+  if (!ctx) return NITI_ERR_ARG;
+  const int rc = norm_args(ctx, "niti_quantize", type, M, C, ws, ws_bytes, NITI_OP_QUANTIZE);
+  if (rc != NITI_OK || M == 0) return rc;
+  if (!x || !q || !s || misaligned(x, (uintptr_t)niti_type_size(type)) || misaligned(s, 4) ||
+      (round_mode != NITI_ROUND_PSR && round_mode != NITI_ROUND_NEAREST))
+    return niti_fail(ctx, NITI_ERR_ARG, "niti_quantize: bad argument (pointers are aligned to their type)");
+  if (round_mode == NITI_ROUND_PSR && type != NITI_F32)
+    return niti_fail(ctx, NITI_ERR_ARG, "niti_quantize: 16-bit values have too few discarded bits for pseudo-stochastic rounding");
+  const NormCall c = {x, nullptr, nullptr, nullptr, q, s, nullptr, type, M, C, row_exponents, round_mode, 0.0f};
+  return run_norm<false>(ctx, (cudaStream_t)stream, c, ws);
+}
+
+extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, const void *h, const float *gain, const float *rstd, const void *dh,
+                                void *dx, float *dgain, int type, int M, int C, void *ws, size_t ws_bytes) {
+  if (!ctx) return NITI_ERR_ARG;
+  int rc = norm_args(ctx, "niti_rmsnorm_bwd", type, M, C, ws, ws_bytes, NITI_OP_RMSNORM_BWD);
+  if (rc != NITI_OK) return rc;
+  cudaStream_t st = (cudaStream_t)stream;
+  if (misaligned(dgain, 4)) return niti_fail(ctx, NITI_ERR_ARG, "niti_rmsnorm_bwd: bad argument (pointers are aligned to their type)");
+  if (M == 0) {
+    if (dgain) NITI_CUDA_TRY(ctx, cudaMemsetAsync(dgain, 0, (size_t)C * 4, st));
+    return NITI_OK;
+  }
+  const uintptr_t es = (uintptr_t)niti_type_size(type);
+  if (!dy || !h || !gain || !rstd || !dx || (((uintptr_t)dy | (uintptr_t)h | (uintptr_t)dh | (uintptr_t)dx) & (es - 1)) ||
+      (((uintptr_t)gain | (uintptr_t)rstd) & 3))
+    return niti_fail(ctx, NITI_ERR_ARG, "niti_rmsnorm_bwd: bad argument (pointers are aligned to their type)");
+  float *part = dgain ? (float *)((char *)ws + NITI_WS_HEADER) : nullptr;
+  const bool aligned = (((uintptr_t)dy | (uintptr_t)h | (uintptr_t)dh | (uintptr_t)dx) & 15) == 0;
+  const RowPlan pl = plan_rows(M, C, type, aligned, 4);
+  int nparts = 0;
+  rc = with_type(type, [&](auto t) -> int {
+    constexpr int T = decltype(t)::value;
+    constexpr int V16 = 16 / (int)sizeof(typename FloatOf<T>::type);
+    if (!pl.nv) {
+      if (dgain) {
+        nparts = M < BWD_PARTS ? M : BWD_PARTS;
+        NITI_CUDA_TRY(ctx, niti_launch(st, dim3((unsigned)((C + 255) / 256), (unsigned)nparts), 256, 0, norm_wide_gain_kernel<T>, dy, h, rstd,
+                                       part, M, C));
+        ctx->launches++;
+      }
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(M < 2 * ctx->sm_count ? M : 2 * ctx->sm_count), 1024, 0, norm_bwd_wide_kernel<T>, dy, h, gain,
+                                     rstd, dh, dx, M, C));
+      return NITI_OK;
+    }
+    const int threads = pl.sh.tpr * pl.sh.rpb;
+    unsigned blocks = row_blocks(ctx, pl.sh, threads, 512);
+    if (blocks > BWD_PARTS) blocks = BWD_PARTS;
+    nparts = (int)blocks;
+    const size_t smem = part && pl.sh.rpb > 1 ? (size_t)pl.sh.rpb * C * 4 : 0;       // (at most 8 rows of 1024)
+    auto rows = [&](auto vec, auto nv) -> int {
+      NITI_CUDA_TRY(ctx, niti_launch(st, blocks, threads, smem, norm_bwd_kernel<T, decltype(vec)::value, decltype(nv)::value>, dy, h, gain, rstd, dh,
+                                     dx, part, pl.sh));
+      return NITI_OK;
+    };
+    auto pick = [&](auto vec) -> int {
+      if (pl.nv == 1) return rows(vec, std::integral_constant<int, 1>{});
+      if (pl.nv == 2) return rows(vec, std::integral_constant<int, 2>{});
+      return rows(vec, std::integral_constant<int, 4>{});
+    };
+    return pl.vec == 1 ? pick(std::integral_constant<int, 1>{}) : pick(std::integral_constant<int, V16>{});
+  });
+  ctx->launches++;
+  if (rc != NITI_OK || !dgain) return rc;
+  NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)((C + 31) / 32), 256, 0, gain_sum_kernel, (const float *)part, dgain, nparts, C));
+  ctx->launches++;
+  return NITI_OK;
+}
+
+extern "C" int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, void *out, int format, int exponent_bytes, int type,
+                               int64_t n, int64_t per) {
+  if (!ctx) return NITI_ERR_ARG;
+  if (n == 0 && niti_type_ok(type)) return NITI_OK;
+  if (!q || !s || !out || !niti_type_ok(type) || n < 0 || per < 0 || (format != NITI_I8 && format != NITI_E4M3) ||
+      (exponent_bytes != 1 && exponent_bytes != 4) || misaligned(out, (uintptr_t)niti_type_size(type)) || misaligned(s, (uintptr_t)exponent_bytes))
+    return niti_fail(ctx, NITI_ERR_ARG, "niti_dequantize: bad argument (pointers are aligned to their type)");
+  const bool wide = n % 16 == 0 && per % 16 == 0 && !misaligned(q, 16) && !misaligned(out, 16) && n / 16 < (1LL << 31);
+  const long long items = wide ? n / 16 : n;
+  const long long blocks = (items + 255) / 256, cap = 16LL * ctx->sm_count;
+  const Div d = wide && per ? make_div(per / 16 < (1LL << 31) ? per / 16 : (1LL << 31)) : Div{0u, 0};
+  const int rc = with_type(type, [&](auto t) -> int {
+    constexpr int T = decltype(t)::value;
+    auto go = [&](auto e4m3, auto sv, auto w) -> int {
+      typedef decltype(sv) S;
+      NITI_CUDA_TRY(ctx, niti_launch((cudaStream_t)stream, (unsigned)(blocks < cap ? blocks : cap), 256, 0,
+                                     dequantize_kernel<T, decltype(e4m3)::value, S, decltype(w)::value>, (const uint8_t *)q, (const S *)s, out,
+                                     (long long)n, d, (long long)per));
+      return NITI_OK;
+    };
+    auto by_exponent = [&](auto e4m3, auto w) -> int { return exponent_bytes == 1 ? go(e4m3, (int8_t)0, w) : go(e4m3, (int32_t)0, w); };
+    auto by_width = [&](auto e4m3) -> int { return wide ? by_exponent(e4m3, std::true_type{}) : by_exponent(e4m3, std::false_type{}); };
+    return format == NITI_E4M3 ? by_width(std::true_type{}) : by_width(std::false_type{});
+  });
+  ctx->launches++;
+  return rc;
+}
