@@ -77,11 +77,18 @@ extern "C" {
 #define NITI_OP_RMSNORM_FWD 8 /* dims = {M, C}                    */
 #define NITI_OP_RMSNORM_BWD 9 /* dims = {M, C}                    */
 #define NITI_OP_QUANTIZE 10   /* dims = {M, C}                    */
+#define NITI_OP_LINEAR_ACT_FWD 11 /* dims = {M, N, K}             */
+#define NITI_OP_LINEAR_ACT_BWD 12 /* dims = {M, N, K}             */
 
 /* element types of the float tensors that some calls take */
 #define NITI_F32 0
 #define NITI_BF16 1
 #define NITI_F16 2
+/* activations */
+#define NITI_ACT_NONE 0
+#define NITI_ACT_RELU 1
+#define NITI_ACT_GELU 2       /* z Phi(z), Phi the normal distribution function  */
+#define NITI_ACT_SILU 3       /* z / (1 + exp(-z))                 */
 /* 8-bit formats of niti_dequantize() */
 #define NITI_I8 0             /* int8 payload                     */
 #define NITI_E4M3 1           /* sign, 4 exponent bits (bias 7), 3 fraction bits; codes 127 and 255 do not occur */
@@ -466,6 +473,28 @@ int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t *q, int32_t
  * every exponent (0: one exponent for all); exponents of exponent_bytes = 4 (int32) or 1 (int8). */
 int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, void *out, int format,
                     int exponent_bytes, int type, int64_t n, int64_t per);
+
+/* Fully connected layer whose result leaves the format in the multiply's epilogue:
+ *   z[m][n] = 2^(s_a[m] + s_w) sum_k a[m][k] w[n][k] + bias[n],   out = act(z) + residual.
+ * a [M][K] int8 with one exponent per row (row_exponents != 0) or one; w [N][K] int8 with the exponent *s_w; both 16-byte
+ * aligned, K <= 131072 (int32 sums are then exact).  bias [N] float32, residual [M][N] may be NULL; out, residual and z
+ * (NULL unless a backward pass follows) are of `type`; out may be the storage of the residual.  Exponents are clamped, and
+ * NITI_DEV_EXP_RANGE raised, where s_a + s_w leaves [-128, 127].  No hook of niti_set_reduce_hook() is called: with
+ * exponents per row a row's result depends on nothing else.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
+int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, int row_exponents, const int8_t *w,
+                        const int32_t *s_w, const float *bias, const void *residual, void *out, void *z, int type, int M,
+                        int N, int K, int act, void *ws, size_t ws_bytes);
+
+/* Its backward pass.  With e = dout act'(z) and (e8, s_e) = e rounded to payloads with one exponent for the tensor:
+ *   dbias[n] = sum_m e[m][n] (of e itself, in a fixed order),
+ *   dx[m][k] = 2^(s_e + s_w) sum_n e8[m][n] w[n][k],    dw[n][k] = 2^(s_e + s_a) sum_m e8[m][n] a[m][k].
+ * The gradient of the residual is dout.  a has ONE exponent here (the sum over m cannot take out more); M and N at most
+ * 131072.  dout, z and dx are of `type`, dw of dw_type; z may be NULL without an activation; dx, dw and dbias may be NULL;
+ * dx may be the storage of dout or z.  round_mode 0 is refused where e has only the bits of a 16-bit type (no activation,
+ * or NITI_ACT_RELU).  Workspace: NITI_OP_LINEAR_ACT_BWD. */
+int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, const int8_t *w,
+                        const int32_t *s_w, const void *z, const void *dout, void *dx, void *dw, float *dbias, int type,
+                        int dw_type, int M, int N, int K, int act, int round_mode, void *ws, size_t ws_bytes);
 
 /* One AdamW step over n tensors (a host array that the call reads before it returns; two of them must not share
  * memory).  With t = *step, the number of this step (device int32, >= 1: a captured graph counts it up between its

@@ -17,7 +17,8 @@ OK, ERR_ARG, ERR_SHAPE, ERR_WORKSPACE, ERR_RANGE, ERR_CUDA, ERR_DEVICE = range(7
 ROUND_PSR, ROUND_NEAREST = 0, 1
 OP_LINEAR_FWD, OP_LINEAR_BWD, OP_CONV_FWD, OP_CONV_DGRAD, OP_CONV_WGRAD, OP_INT_XENT = range(6)
 OP_LINEAR_BWD_UPDATE, OP_CONV_WGRAD_UPDATE = 6, 7
-OP_RMSNORM_FWD, OP_RMSNORM_BWD, OP_QUANTIZE = 8, 9, 10
+OP_RMSNORM_FWD, OP_RMSNORM_BWD, OP_QUANTIZE, OP_LINEAR_ACT_FWD, OP_LINEAR_ACT_BWD = 8, 9, 10, 11, 12
+_ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 F32, BF16, F16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 I8, E4M3 = 0, 1
@@ -35,6 +36,7 @@ EXPORTS = [
     "niti_copy_tensors", "niti_relu_fwd",
     "niti_relu_bwd", "niti_maxpool2_fwd", "niti_maxpool2_bwd", "niti_maxpool2_fwd_idx", "niti_maxpool2_bwd_idx",
     "niti_rmsnorm_fwd", "niti_rmsnorm_bwd", "niti_quantize", "niti_dequantize", "niti_adamw",
+    "niti_linear_act_fwd", "niti_linear_act_bwd",
 ]
 
 
@@ -116,6 +118,8 @@ def load_library():
     lib.niti_rmsnorm_bwd.argtypes = [vp] * 9 + [i32, i32, i32, vp, sz]
     lib.niti_quantize.argtypes = [vp] * 5 + [i32, i32, i32, i32, i32, vp, sz]
     lib.niti_dequantize.argtypes = [vp] * 5 + [i32, i32, i32, i64, i64]
+    lib.niti_linear_act_fwd.argtypes = [vp, vp, vp, vp, i32] + [vp] * 6 + [i32] * 5 + [vp, sz]
+    lib.niti_linear_act_bwd.argtypes = [vp] * 11 + [i32] * 7 + [vp, sz]
     lib.niti_adamw.argtypes = [vp, vp, C.POINTER(_AdamwTensor), i32, i32, vp, f64, f64, f64, f64, vp]
     return lib
 
@@ -632,6 +636,53 @@ class Niti:
         self._ck(self.lib.niti_dequantize(self.h, self._stream(), _ptr(q), _ptr(s), _ptr(out),
                                           I8 if q.dtype == torch.int8 else E4M3, s.element_size(), _TYPES[dtype], n, per or 0))
         return out
+
+    def linear_act_fwd(self, a, s_a, w, s_w, bias=None, residual=None, act="none", out=None, z=None, keep_z=False,
+                       dtype=torch.bfloat16):
+        """niti_linear_act_fwd: (out, z); z, the argument of the activation, is None unless ``keep_z`` (or a tensor for it) is
+        given.  ``s_a``: [M] exponents, or [1]; ``act``: "none", "relu", "gelu" or "silu"."""
+        self._tensor(a, "a", None, torch.int8)
+        if a.dim() != 2 or act not in _ACTS or dtype not in _TYPES:
+            raise NitiError(ERR_ARG, "linear_act_fwd: a matrix, a known activation and a float type are needed")
+        M, K = a.shape
+        N = w.shape[0]
+        self._tensor(w, "w", (N, K), torch.int8)
+        rows = s_a.numel() != 1
+        self._tensor(s_a, "s_a", (M,) if rows else None, torch.int32)
+        self._tensor(s_w, "s_w", (1,), torch.int32)
+        if bias is not None:
+            self._tensor(bias, "bias", (N,), torch.float32)
+        if residual is not None:
+            self._tensor(residual, "residual", (M, N), dtype)
+        out = self._out(out, "out", (M, N), dtype)
+        z = self._out(z, "z", (M, N), dtype) if keep_z or z is not None else None
+        ws, wsb = self._ws_for(OP_LINEAR_ACT_FWD, M, N, K)
+        self._ck(self.lib.niti_linear_act_fwd(self.h, self._stream(), _ptr(a), _ptr(s_a), int(rows), _ptr(w), _ptr(s_w), _ptr(bias),
+                                              _ptr(residual), _ptr(out), _ptr(z), _TYPES[dtype], M, N, K, _ACTS[act], ws, wsb))
+        return out, z
+
+    def linear_act_bwd(self, a, s_a, w, s_w, dout, z=None, act="none", need_dx=True, dx=None, dw=None, dbias=None,
+                       dw_dtype=torch.float32, round_mode=ROUND_NEAREST):
+        """niti_linear_act_bwd: (dx, dw, dbias); dx is None unless ``need_dx``.  a has one exponent."""
+        type_id = self._float(dout, "dout")
+        M, N = dout.shape
+        if act not in _ACTS or dw_dtype not in _TYPES or a.dim() != 2:
+            raise NitiError(ERR_ARG, "linear_act_bwd: a matrix, a known activation and a float type are needed")
+        K = a.shape[1]
+        self._tensor(a, "a", (M, K), torch.int8)
+        self._tensor(w, "w", (N, K), torch.int8)
+        self._tensor(s_a, "s_a", (1,), torch.int32)
+        self._tensor(s_w, "s_w", (1,), torch.int32)
+        if z is not None:
+            self._tensor(z, "z", dout.shape, dout.dtype)
+        dx = self._out(dx, "dx", (M, K), dout.dtype) if need_dx else None
+        dw = self._out(dw, "dw", (N, K), dw_dtype)
+        dbias = self._out(dbias, "dbias", (N,), torch.float32)
+        ws, wsb = self._ws_for(OP_LINEAR_ACT_BWD, M, N, K)
+        self._ck(self.lib.niti_linear_act_bwd(self.h, self._stream(), _ptr(a), _ptr(s_a), _ptr(w), _ptr(s_w), _ptr(z), _ptr(dout),
+                                              _ptr(dx), _ptr(dw), _ptr(dbias), type_id, _TYPES[dw_dtype], M, N, K, _ACTS[act],
+                                              round_mode, ws, wsb))
+        return dx, dw, dbias
 
     def adamw_state(self, p, bits=8):
         """Fresh states of a weight tensor for ``adamw_tensors``: (m, v, s_m, s_v), the exponents None with 32 bits."""

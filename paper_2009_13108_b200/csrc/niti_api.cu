@@ -3,6 +3,7 @@
 #include "niti_common.cuh"
 
 size_t niti_norm_ws_bytes(int op, long long M, long long C);
+size_t niti_linear_act_ws_bytes(int op, long long M, long long N, long long K);
 int niti_launch_im2col32(niti_ctx *ctx, cudaStream_t st, const int8_t *x, int8_t *xcol, int B, int H, int W,
                          int Ci, int R, int S, int pad, int stride, int Ho, int Wo);
 int niti_launch_widen(niti_ctx *ctx, cudaStream_t st, const int8_t *x, int8_t *xw, int rows, int W, int Ci, int Cp, int pad,
@@ -403,6 +404,10 @@ extern "C" size_t niti_workspace_bytes(int op, const int64_t *d, int nd) {
     case NITI_OP_QUANTIZE:
       if (nd != 2 || d[0] < 0 || d[1] <= 0) return 0;
       return niti_norm_ws_bytes(op, d[0], d[1]);
+    case NITI_OP_LINEAR_ACT_FWD:
+    case NITI_OP_LINEAR_ACT_BWD:
+      if (nd != 3 || d[0] < 0 || d[1] <= 0 || d[2] <= 0) return 0;
+      return niti_linear_act_ws_bytes(op, d[0], d[1], d[2]);
     default:
       return 0;
   }

@@ -1,0 +1,22 @@
+// Internal interface of the fully connected layers with a float epilogue.
+#pragma once
+#include "niti_common.cuh"
+
+// out = act(sum * 2^(s0 + s1) + bias) + res; z (optional) receives the argument of act.
+struct LinearEpilogue {
+  const int32_t *s0;       // exponents: one, or (s0_rows) one for every row of the output
+  const int32_t *s1;       // one
+  const float *bias;       // per column, may be null
+  const void *res;         // may be null
+  void *out, *z;           // z may be null
+  int s0_rows, act;
+};
+
+// Contractions are split only where all shares run at once, so that their sums take at most a tile of 128 x 256 words an SM.
+#define NITI_LINEAR_MAX_SMS 160
+// One multiply on the tensor cores; operands with 16-byte aligned rows of pitch ld0, ld1.  kind: GK_FC_FWD (A [gm][gk], B
+// [gn][gk]), GK_FC_DGRAD (A [gm][gk], B [gk][gn]) or GK_FC_WGRAD (A [gk][gm], B [gk][gn]).  counters: NITI_LINEAR_COUNTERS
+// zeroed words; next: a header to be zeroed for a later call, or null.
+#define NITI_LINEAR_COUNTERS 320
+int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0, long long ld0, const int8_t *p1, long long ld1, long long gm,
+                     long long gn, long long gk, const LinearEpilogue &e, int type, int *slabs, unsigned *counters, WsHeader *next);

@@ -210,7 +210,7 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
 
 // Backward: with G = gain dy and c = sum_c(G h) r^3 / C:  dx = dh + r G - c h;  dgain = sum over the rows of dy h r.  The
 // columns of a thread are the same in every row, so the gain's gradient stays in its registers; each block leaves its sums
-// in `part` and gain_sum_kernel adds them up in a fixed order.
+// in `part` and column_sum_kernel adds them up in a fixed order.
 template <int T, int VEC, int NV>
 __global__ void __launch_bounds__(ROW_MOST)
 norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, float *part,
@@ -351,7 +351,7 @@ norm_wide_gain_kernel(const void *dy, const void *h, const float *rstd, float *p
 
 // dst[c] = sum over the rows of part[n][C]: 32 columns a block, eight threads a column.
 __global__ void __launch_bounds__(256)
-gain_sum_kernel(const float *part, float *dst, int n, int C) {
+column_sum_kernel(const float *part, float *dst, int n, int C) {
   __shared__ float buf[8][33];
   niti_enter(part);
   const int tx = (int)threadIdx.x & 31, ty = (int)threadIdx.x >> 5;
@@ -570,6 +570,8 @@ extern "C" int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t 
   return run_norm<false>(ctx, (cudaStream_t)stream, c, ws);
 }
 
+int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C);
+
 extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, const void *h, const float *gain, const float *rstd, const void *dh,
                                 void *dx, float *dgain, int type, int M, int C, void *ws, size_t ws_bytes) {
   if (!ctx) return NITI_ERR_ARG;
@@ -622,7 +624,12 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
   });
   ctx->launches++;
   if (rc != NITI_OK || !dgain) return rc;
-  NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)((C + 31) / 32), 256, 0, gain_sum_kernel, (const float *)part, dgain, nparts, C));
+  return niti_launch_column_sums(ctx, st, part, dgain, nparts, C);
+}
+
+// dst[c] = sum over n rows of part[n][C], in a fixed order
+int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C) {
+  NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)((C + 31) / 32), 256, 0, column_sum_kernel, part, dst, n, C));
   ctx->launches++;
   return NITI_OK;
 }
