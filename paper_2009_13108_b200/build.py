@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libniti_b200.so")
 SOURCES = ["niti_api.cu", "niti_elementwise.cu", "niti_simt_gemm.cu", "niti_small_gemm.cu", "niti_tc_gemm.cu",
-           "niti_norm.cu", "niti_adamw.cu", "niti_linear_act.cu"]
+           "niti_norm.cu", "niti_adamw.cu", "niti_linear_act.cu", "niti_linear_rows.cu"]
 
 
 def _newest_source() -> float:

@@ -48,6 +48,11 @@ __device__ __forceinline__ void split_e4m3(float t, unsigned &code, unsigned &re
   code = normal ? (b >> 20) - 960u : small >> 16;
   rest = (normal ? b >> 4 : small) & 0xffffu;
 }
+__device__ __forceinline__ float root(float x) {                      // (within two steps of 2^-24)
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 __device__ __forceinline__ float value_e4m3(unsigned code) {          // of a code without its sign
   return __uint_as_float(code << 20) * 1.329227995784916e+36f;        // 2^120
 }
@@ -169,7 +174,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
         m[j] = fmaf(hy.b1, m[j], hy.c1 * gj);
         v[j] = fmaf(hy.b2, v[j], hy.c2 * gj * gj);
       }
-      r[j] = sqrtf(v[j]);
+      r[j] = root(v[j]);
       if (ok) p[j] = fmaf(p[j], decay, -lr_m * __fdividef(m[j], fmaf(r[j], rs_v, hy.eps)));
       bad |= !ok;
     }

@@ -70,6 +70,43 @@ struct Pack {
   }
 };
 
+// 32 bytes, a whole sector (pointers 32-byte aligned)
+__device__ __forceinline__ void load32(const void *src, unsigned (&w)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(src)
+               : "memory");
+}
+__device__ __forceinline__ void store32(void *dst, const unsigned (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+// 32 bytes of a type from (and to) 32 / size floats
+template <int T, int N>
+__device__ __forceinline__ void pack32(const float *v, unsigned (&w)[8]) {
+  static_assert(N == 32 / (int)sizeof(typename FloatOf<T>::type), "");
+  constexpr int V = N / 2;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float part[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) part[j] = v[V * h + j];
+    Pack<T, V> k;
+    k.set(part);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[4 * h + j] = k.w[j];
+  }
+}
+template <int T, int N>
+__device__ __forceinline__ float get32(const unsigned (&w)[8], int j) {
+  constexpr int V = N / 2;
+  Pack<T, V> k;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) k.w[i] = w[4 * (j / V) + i];
+  return k.get(j % V);
+}
+
 // ---- rounding to payloads -------------------------------------------------------------------
 // Exponent of a tensor (or row) whose largest magnitude has these bits: the one that leaves seven integer bits, so that
 // payload magnitudes reach 64 .. 127 (the effective bit-width rule of Section 3.2 on floats).  Not below NITI_EXP_LOWEST

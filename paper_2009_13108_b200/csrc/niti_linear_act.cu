@@ -46,43 +46,6 @@ __device__ __forceinline__ void decode(const Params &p, int item, int &mu, int &
   mu = g * p.raster_g + rem - nt * (last ? p.m_units - g * p.raster_g : p.raster_g);
 }
 
-// 32 bytes of a row
-__device__ __forceinline__ void load32(const void *src, unsigned (&w)[8]) {
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-               : "l"(src)
-               : "memory");
-}
-__device__ __forceinline__ void store32(void *dst, const unsigned (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-               ::"l"(dst), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-// 32 bytes of a type from (and to) 32 / size floats
-template <int T, int N>
-__device__ __forceinline__ void pack32(const float *v, unsigned (&w)[8]) {
-  static_assert(N == 32 / (int)sizeof(typename FloatOf<T>::type), "");
-  constexpr int V = N / 2;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float part[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) part[j] = v[V * h + j];
-    Pack<T, V> k;
-    k.set(part);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[4 * h + j] = k.w[j];
-  }
-}
-template <int T, int N>
-__device__ __forceinline__ float get32(const unsigned (&w)[8], int j) {
-  constexpr int V = N / 2;
-  Pack<T, V> k;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) k.w[i] = w[4 * (j / V) + i];
-  return k.get(j % V);
-}
-
 // What follows the multiply, for 32 columns from n0 of a tile's rows; a lane holds the int32 sums of its row.
 template <int T>
 __device__ __forceinline__ void finish_chunk(const Params &p, int (&v)[32], int row0, int n0, float f, float *stg, int lane) {
@@ -600,8 +563,8 @@ constexpr int ERR_THREADS = 128;
 constexpr unsigned INF_BITS = 0x7f800000u;
 
 // e = dout act'(z) of a block's rows and columns, a thread on the same VEC columns in every row.
-template <int T, int VEC, typename F>
-__device__ __forceinline__ void error_rows(const void *dout, const void *z, int act, int N, int r0, int r1, int c, F take) {
+template <int T, int VEC, int ACT, typename F>
+__device__ __forceinline__ void error_rows(const void *dout, const void *z, int N, int r0, int r1, int c, F take) {
   constexpr int DEEP = 4;                          // rows in flight
   for (int r = r0; r < r1; r += DEEP) {
     Pack<T, VEC> d[DEEP], zz[DEEP];
@@ -609,14 +572,14 @@ __device__ __forceinline__ void error_rows(const void *dout, const void *z, int 
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
         d[k].load(dout, (long long)(r + k) * N + c);
-        if (act != NITI_ACT_NONE) zz[k].load(z, (long long)(r + k) * N + c);
+        if (ACT != NITI_ACT_NONE) zz[k].load(z, (long long)(r + k) * N + c);
       }
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
         float e[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) e[j] = act == NITI_ACT_NONE ? d[k].get(j) : d[k].get(j) * act_slope(zz[k].get(j), act);
+        for (int j = 0; j < VEC; ++j) e[j] = ACT == NITI_ACT_NONE ? d[k].get(j) : d[k].get(j) * act_slope(zz[k].get(j), ACT);
         take(r + k, e);
       }
   }
@@ -624,9 +587,9 @@ __device__ __forceinline__ void error_rows(const void *dout, const void *z, int 
 
 // Largest |e| of the tensor, and the column sums of every block's rows.  Bound: HBM (dout and z are read once here; the
 // rounding pass finds what fits of them in L2).
-template <int T, int VEC>
+template <int T, int VEC, int ACT>
 __global__ void __launch_bounds__(ERR_THREADS)
-error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int act, int M, int N, int rows) {
+error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int M, int N, int rows) {
   niti_enter(dout, z);
   const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = (int)blockIdx.y * rows, r1 = min(r0 + rows, M);
   if (next && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) niti_zero_header(next, (int)threadIdx.x);
@@ -635,7 +598,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 #pragma unroll
   for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
   if (c < N) {
-    error_rows<T, VEC>(dout, z, act, N, r0, r1, c, [&](int, const float (&e)[VEC]) {
+    error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int, const float (&e)[VEC]) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         sum[j] += e[j];
@@ -652,9 +615,9 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 }
 
 // e as payload with the exponent of its maximum, rows of `pitch` bytes.  The rows that the pass before read last come first.
-template <int T, int VEC>
+template <int T, int VEC, int ACT>
 __global__ void __launch_bounds__(ERR_THREADS)
-error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int act, int M, int N, int rows,
+error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, int rows,
                    int pitch, int round_mode) {
   niti_enter(dout, z, hdr);
   const unsigned most = hdr->maxabs32;
@@ -667,7 +630,7 @@ error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, co
   const int by = (int)(gridDim.y - 1 - blockIdx.y);
   const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * rows, r1 = min(r0 + rows, M);
   if (c >= N) return;
-  error_rows<T, VEC>(dout, z, act, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
+  error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
     int q[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) q[j] = niti_payload(e[j], scale, round_mode);
@@ -729,6 +692,8 @@ extern "C" int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a,
       (((uintptr_t)residual | (uintptr_t)out | (uintptr_t)z) & (es - 1)) || z == out || (z && z == residual))
     return niti_fail(ctx, NITI_ERR_ARG, "niti_linear_act_fwd: bad argument (z has a place of its own; pointers are aligned to their type)");
   cudaStream_t st = (cudaStream_t)stream;
+  const LinearEpilogue e = {s_a, s_w, bias, residual, out, z, row_exponents ? 1 : 0, act};
+  if (M <= NITI_LINEAR_ROWS) return niti_linear_rows(ctx, st, a, w, M, N, K, e, type);
   int8_t *pad = (int8_t *)ws + NITI_WS_HEADER;
   int *slabs = (int *)(pad + pad_bytes(M, K) + pad_bytes(N, K));
   const int pitch = (int)pitch16(K);
@@ -740,7 +705,6 @@ extern "C" int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a,
   }
   WsHeader *hdr = niti_take_header(ctx, st, ws), *next = nullptr;
   if ((rc = niti_clear(ctx, st, nullptr, 0, &next)) != NITI_OK) return rc;
-  const LinearEpilogue e = {s_a, s_w, bias, residual, out, z, row_exponents ? 1 : 0, act};
   rc = niti_linear_gemm(ctx, st, GK_FC_FWD, a, pitch, w, pitch, M, N, K, e, type, slabs, niti_split_max(hdr), next);
   if (rc == NITI_OK) niti_header_passed_on(ctx, next);
   return rc;
@@ -777,18 +741,25 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
   const int rows = (M + nblk - 1) / nblk;
   const int v16 = 16 / (int)es;
   const bool vec = N % v16 == 0 && (((uintptr_t)dout | (uintptr_t)z) & 15) == 0;
-  const int zact = act;
-  auto passes = [&](auto tc, auto vc) -> int {
-    constexpr int T = decltype(tc)::value, VEC = decltype(vc)::value;
+  auto passes_as = [&](auto tc, auto vc, auto ac) -> int {
+    constexpr int T = decltype(tc)::value, VEC = decltype(vc)::value, ACT = decltype(ac)::value;
     const dim3 grid((unsigned)((N + ERR_THREADS * VEC - 1) / (ERR_THREADS * VEC)), (unsigned)((M + rows - 1) / rows));
-    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_max_kernel<T, VEC>, dout, z, dbias ? part : (float *)nullptr, hdr, next, zact, M, N, rows));
+    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_max_kernel<T, VEC, ACT>, dout, z, dbias ? part : (float *)nullptr, hdr, next, M, N, rows));
     ctx->launches++;
     niti_header_passed_on(ctx, next);
     if (!dx && !dw) return NITI_OK;
-    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_round_kernel<T, VEC>, dout, z, e8, s_e, (const WsHeader *)hdr, ctx->d_status, zact, M,
+    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT>, dout, z, e8, s_e, (const WsHeader *)hdr, ctx->d_status, M,
                                    N, rows, pitch_e, round_mode));
     ctx->launches++;
     return NITI_OK;
+  };
+  auto passes = [&](auto tc, auto vc) -> int {
+    switch (act) {
+      case NITI_ACT_RELU: return passes_as(tc, vc, std::integral_constant<int, NITI_ACT_RELU>{});
+      case NITI_ACT_GELU: return passes_as(tc, vc, std::integral_constant<int, NITI_ACT_GELU>{});
+      case NITI_ACT_SILU: return passes_as(tc, vc, std::integral_constant<int, NITI_ACT_SILU>{});
+      default: return passes_as(tc, vc, std::integral_constant<int, NITI_ACT_NONE>{});
+    }
   };
   auto by_type = [&](auto tc) -> int {
     constexpr int T = decltype(tc)::value;

@@ -18,5 +18,8 @@ struct LinearEpilogue {
 // [gn][gk]), GK_FC_DGRAD (A [gm][gk], B [gk][gn]) or GK_FC_WGRAD (A [gk][gm], B [gk][gn]).  counters: NITI_LINEAR_COUNTERS
 // zeroed words; next: a header to be zeroed for a later call, or null.
 #define NITI_LINEAR_COUNTERS 320
+// The forward multiply of at most NITI_LINEAR_ROWS rows: streams the weights, in the caller's layout whatever K is.
+#define NITI_LINEAR_ROWS 32
+int niti_linear_rows(niti_ctx *ctx, cudaStream_t st, const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue &e, int type);
 int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0, long long ld0, const int8_t *p1, long long ld1, long long gm,
                      long long gn, long long gk, const LinearEpilogue &e, int type, int *slabs, unsigned *counters, WsHeader *next);
