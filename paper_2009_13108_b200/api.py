@@ -22,6 +22,7 @@ _ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 F32, BF16, F16 = 0, 1, 2
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 I8, E4M3 = 0, 1
+_FORMATS, _EXPONENTS = {torch.int8: I8, torch.uint8: E4M3}, {torch.int32: 4, torch.int8: 1}
 STATE_BLOCK = 256
 REDUCE_MAX_U32, REDUCE_MAX_U64, REDUCE_SUM_I32, REDUCE_SCATTER_SUM_I32, ALLGATHER_I8 = 0, 1, 2, 3, 4
 _REDUCE_FN = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int)
@@ -154,6 +155,7 @@ class Niti:
             raise NitiError(ERR_CUDA, "no CUDA device: this library has no CPU path")
         self.lib = load_library()
         self.device = torch.device("cuda", device)
+        self._gpu = device
         h = C.c_void_p()
         rc = self.lib.niti_create(C.byref(h), device)
         if rc != OK:
@@ -551,41 +553,45 @@ class Niti:
     # ---- float tensors at the boundary of the format ----
     def _tensor(self, t, name, shape=None, dtype=None):
         """An operand the library may be given the pointer of, or NitiError."""
-        if t.get_device() != self.device.index or not t.is_contiguous():
-            raise NitiError(ERR_ARG, "%s: a contiguous tensor on %s is needed" % (name, self.device))
-        if dtype is not None and t.dtype != dtype:
-            raise NitiError(ERR_ARG, "%s: %s needed, got %s" % (name, dtype, t.dtype))
-        if shape is not None and t.shape != shape:
-            raise NitiError(ERR_ARG, "%s: shape %s needed, got %s" % (name, tuple(shape), tuple(t.shape)))
-        return t
+        if (t.get_device() == self._gpu and t.is_contiguous() and (dtype is None or t.dtype is dtype) and
+                (shape is None or t.shape == shape)):
+            return t
+        raise NitiError(ERR_ARG, "%s: a contiguous tensor on %s is needed, %s %s; got %s %s on %s" % (
+            name, self.device, dtype or "of a type that the call takes", "" if shape is None else tuple(shape), t.dtype, tuple(t.shape), t.device))
 
     def _float(self, t, name):
         """(type id) of an activation tensor."""
-        self._tensor(t, name)
-        if t.dtype not in _TYPES or t.dim() != 2:
+        type_id = _TYPES.get(t.dtype)
+        if type_id is None or t.dim() != 2:
             raise NitiError(ERR_ARG, "%s: a matrix of float32, bfloat16 or float16 is needed" % name)
-        return _TYPES[t.dtype]
+        if t.get_device() != self._gpu or not t.is_contiguous():
+            self._tensor(t, name)
+        return type_id
+
+    def _new(self, shape, dtype):
+        """A new output.  (With its strides spelled out torch takes 1.5 us, through torch.empty 2.4: small calls take 10.)"""
+        if len(shape) == 2:
+            return torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
+        return torch.empty_strided(shape, (1,), dtype=dtype, device=self.device)
 
     def _out(self, t, name, shape, dtype):
         """A caller's output after its check, or a new one."""
-        if t is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        return self._tensor(t, name, shape, dtype)
+        return self._new(shape, dtype) if t is None else self._tensor(t, name, shape, dtype)
 
     def rmsnorm_fwd(self, x, gain, residual=None, h=None, y=None, s_y=None, rstd=None, rows=True, eps=1e-6,
                     round_mode=ROUND_NEAREST):
         """niti_rmsnorm_fwd: (payload, exponents [M] or with ``rows=False`` [1], h = x + residual, 1 / rms).  Without a
         residual h is x."""
         type_id = self._float(x, "x")
-        M, Cc = x.shape
+        shape = M, Cc = x.shape
         self._tensor(gain, "gain", (Cc,), torch.float32)
         if residual is None:
             if h is not None:
                 raise NitiError(ERR_ARG, "h: written only with a residual")
         else:
-            self._tensor(residual, "residual", x.shape, x.dtype)
-            h = self._out(h, "h", x.shape, x.dtype)
-        y = self._out(y, "y", x.shape, torch.int8)
+            self._tensor(residual, "residual", shape, x.dtype)
+            h = self._out(h, "h", shape, x.dtype)
+        y = self._out(y, "y", shape, torch.int8)
         s_y = self._out(s_y, "s_y", (M if rows else 1,), torch.int32)
         rstd = self._out(rstd, "rstd", (M,), torch.float32)
         ws, wsb = self._ws_for(OP_RMSNORM_FWD, M, Cc)
@@ -625,16 +631,22 @@ class Niti:
         one per row of ``q``, or one for every ``block`` elements (the last block may be short)."""
         self._tensor(q, "q")
         self._tensor(s, "s")
-        n, per = q.numel(), block
-        if per is None and s.numel() != 1:
-            per = q.shape[-1]
-        if q.dtype not in (torch.int8, torch.uint8) or s.dtype not in (torch.int32, torch.int8) or dtype not in _TYPES:
+        n, per, count, type_id = q.numel(), block, s.numel(), _TYPES.get(dtype)
+        form, size = _FORMATS.get(q.dtype), _EXPONENTS.get(s.dtype)
+        if form is None or size is None or type_id is None:
             raise NitiError(ERR_ARG, "dequantize: int8 or uint8 elements, int32 or int8 exponents, a float result")
-        if s.numel() != (1 if per is None else -(-n // per) if per > 0 else -1) and n:
-            raise NitiError(ERR_ARG, "dequantize: %d exponents for %d elements, %s each" % (s.numel(), n, per or "all"))
-        out = self._out(out, "out", q.shape, dtype)
-        self._ck(self.lib.niti_dequantize(self.h, self._stream(), _ptr(q), _ptr(s), _ptr(out),
-                                          I8 if q.dtype == torch.int8 else E4M3, s.element_size(), _TYPES[dtype], n, per or 0))
+        if per is None:
+            per = 0 if count == 1 else q.shape[-1]
+        if n and count != (-(-n // per) if per > 0 else 1 if block is None else -1):
+            raise NitiError(ERR_ARG, "dequantize: %d exponents for %d elements, %s each" % (count, n, per or "all"))
+        if out is None and q.dim() <= 2:
+            out = self._new(q.shape, dtype)
+        elif out is None:
+            out = torch.empty(q.shape, dtype=dtype, device=self.device)
+        else:
+            self._tensor(out, "out", q.shape, dtype)
+        self._ck(self.lib.niti_dequantize(self.h, self._stream(), q.data_ptr(), s.data_ptr(), out.data_ptr(), form, size, type_id,
+                                          n, per))
         return out
 
     def linear_act_fwd(self, a, s_a, w, s_w, bias=None, residual=None, act="none", out=None, z=None, keep_z=False,

@@ -2,6 +2,7 @@
 // Bound: HBM.  A parameter moves 8 bytes of weight, its gradient, its states twice (2 x 8 bytes, or 2 x 2) and a byte of
 // working copy; all of a network's tensors share launches, and a tensor list travels with the launch.
 #include "niti_float.cuh"
+#include "niti_tcgen05.cuh"
 #include <math.h>
 
 namespace {
@@ -9,6 +10,12 @@ namespace {
 constexpr int BLOCK = NITI_STATE_BLOCK;            // elements that share the exponent of an 8-bit state: a warp's share
 static_assert(BLOCK == 256, "eight elements a lane");
 constexpr int WARPS = 8;
+constexpr int CHUNK = WARPS * BLOCK;               // elements that a CTA works on at a time
+constexpr int STAGES = 3;
+constexpr int GROUP = 4;                           // chunks that a CTA takes in a row where there are many
+// bytes of a chunk in shared memory: weights, gradients (room for 32 bits), both states
+__host__ __device__ constexpr int stage_bytes(bool eight) { return CHUNK * (4 + 4 + (eight ? 2 : 8)); }
+__host__ __device__ constexpr int ctas_per_sm(bool eight) { return eight ? 3 : 2; }
 constexpr int LIST_SMALL = 16, LIST_MOST = 256;    // tensors a launch takes (its parameters: 1.4 and 22 KB)
 
 struct Tensor {
@@ -19,18 +26,18 @@ struct Tensor {
   const int32_t *s_w;
   long long n;
   float decay;                                     // 1 - lr * weight decay
-  short g_type, vec;                               // vec: every pointer allows vectors of eight elements
+  short g_type, vec;                               // vec: whole chunks may be copied to shared memory in bulk
 };
 template <int MOST>
 struct List {
   int n;
-  int first[MOST + 1];                             // first chunk of each tensor
+  int first[MOST + 1];                             // first group of each tensor, all tensors' groups counted through
   Tensor t[MOST];
 };
 struct Hyper {
-  float lr, b1, b2, c1, c2, eps;                   // c = 1 - b
+  float lr, b1, b2, root_b2, c1, c2, eps;          // c = 1 - b
   float log_b1, log_b2;
-  int blocks;                                      // 256-element blocks of a chunk
+  int group;                                       // chunks of a group
 };
 
 __device__ __forceinline__ float load_grad(const void *g, int type, long long i) {
@@ -39,24 +46,44 @@ __device__ __forceinline__ float load_grad(const void *g, int type, long long i)
   return __half2float(reinterpret_cast<const __half *>(g)[i]);
 }
 
-// A scaled magnitude t < 256 as a code of three fraction bits, rounded down, and the 16 bits behind it.  Below 2^-6 codes
-// are multiples of 2^-9.
-__device__ __forceinline__ void split_e4m3(float t, unsigned &code, unsigned &rest) {
-  const unsigned b = __float_as_uint(t);
-  const unsigned small = __float2uint_rz(t * 33554432.0f);            // t 2^9 2^16
-  const bool normal = b >= (121u << 23);
-  code = normal ? (b >> 20) - 960u : small >> 16;
-  rest = (normal ? b >> 4 : small) & 0xffffu;
-}
-__device__ __forceinline__ float root(float x) {                      // (within two steps of 2^-24)
+__device__ __forceinline__ float root(float x) {                      // (within a few steps of 2^-24; 0 for subnormal numbers)
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-__device__ __forceinline__ float value_e4m3(unsigned code) {          // of a code without its sign
-  return __uint_as_float(code << 20) * 1.329227995784916e+36f;        // 2^120
+__device__ __forceinline__ float reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
-
+// In bits 20 .. 27, the code below a magnitude t < 256, given as t 2^-24, plus what 16 random bits (times 16: `sixteen` is 16
+// in a register, which keeps the multiply-add from becoming a shift and an addition on the busier integer pipe) carry into it.
+// The last four bits of a float's exponent and its first three fraction bits are the code: exponent fields of codes 8 .. 120
+// (2^-6 .. 2^8) end in 00001 .. 01111 after the multiplication by 2^-24.  SMALL: below 2^-6, where codes are multiples of
+// 2^-9, adding 2^-6 puts the number into a binade with that spacing, eight codes too high.
+constexpr float LEAST_NORMAL = 9.313225746154785e-10f;                  // 2^-6 2^-24
+constexpr float LEAST_CODE = 1.1641532182693481e-10f;                   // 2^-9 2^-24
+template <bool SMALL>
+__device__ __forceinline__ unsigned draw_e4m3(float t, unsigned draw, unsigned sixteen) {
+  unsigned b = __float_as_uint(t);
+  if (SMALL && t < LEAST_NORMAL) b = __float_as_uint(t + LEAST_NORMAL) - (8u << 20);
+  return draw * sixteen + b;
+}
+// The codes of four such words in one
+__device__ __forceinline__ unsigned pack_codes(unsigned a, unsigned b, unsigned c, unsigned d) {
+  return __byte_perm(__byte_perm(a, b, 0x7632) >> 4, __byte_perm(c, d, 0x7632) >> 4, 0x6420);
+}
+// Values of the four codes in a word (the conversion to half precision is exact: 2^-9 .. 448)
+__device__ __forceinline__ void values_e4m3(unsigned w, float (&v)[4]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    unsigned p;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(p) : "h"((unsigned short)(h ? w >> 16 : w & 0xffffu)));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&p));
+    v[2 * h] = f.x;
+    v[2 * h + 1] = f.y;
+  }
+}
 // 32 random bits for an element of a tensor in a step (multiply and shift mixing, constants of C. Wellons' search for
 // 32-bit mixing functions of low bias).
 __device__ __forceinline__ unsigned random_bits(unsigned index, unsigned key) {
@@ -66,193 +93,358 @@ __device__ __forceinline__ unsigned random_bits(unsigned index, unsigned key) {
   return x ^ (x >> 16);
 }
 
-// A warp works on one block of 256 elements at a time, a lane on eight (consecutive ones where the tensor allows vectors,
-// else every 32nd).  8-bit states are codes of the first moment and of the root of the second, r = sqrt(v): the root
-// halves the range that a code has to span, and it is what the step divides by.  Both round stochastically, since to
-// nearest a state that changes by a thousandth a step would never leave its code.  The random bits come from the element's
-// index and the step, not from discarded bits as in the integer calls: m mixes a short code and a short gradient with
-// weights 9/10 and 1/10, whose binary expansions repeat the same four bits, and without a gradient a code meets the same
-// constant, and so the same discarded bits, in every step.  A root that is not zero does not round to zero (the next step
-// divides by it).
-template <int MOST, bool EIGHT>
-__global__ void __launch_bounds__(32 * WARPS)
-adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t *step, const float *grad_scale, uint32_t *status) {
-  niti_enter(step, grad_scale);
-  const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-  int lo = 0, hi = l.n;                            // the tensor of this chunk
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (l.first[mid] <= (int)blockIdx.x) lo = mid; else hi = mid;
+struct Step {                                      // of this step and tensor
+  float b1, root_b2;                               // b1, sqrt(b2)
+  float c1, c2;                                    // (1 - b1) gs, (1 - b2) gs^2 for a gradient scale gs
+  float den_r, den_1;                              // the step is m / (r den_r + den_1)
+  float decay, gs, w_scale;
+  unsigned key, sixteen;
+};
+
+// A warp works on one block of 256 elements at a time, a lane on eight (two vectors of four, or every 32nd element).  8-bit
+// states are codes of the first moment and of the root of the second, r = sqrt(v): the root halves the range that a code has to
+// span, and it is what the step divides by.  Both round stochastically, since to nearest a state that changes by a thousandth a
+// step would never leave its code.  The random bits come from the element's index and the step, not from discarded bits as in
+// the integer calls: m mixes a short code and a short gradient with weights 9/10 and 1/10, whose binary expansions repeat the
+// same four bits, and without a gradient a code meets the same constant, and so the same discarded bits, in every step.  A root
+// that is not zero does not round to zero (the next step divides by it).  s_m, s_v: the block's exponents, before and after.
+// Returns whether a gradient was not finite.
+// VEC: the operands are in shared memory at `stage` (the barrier `empty` is told when they have been read), else everything
+// goes by elements.
+template <bool EIGHT, bool VEC>
+__device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, const Step &st, long long blk, int warp, int lane, int &s_m, int &s_v,
+                                            const char *stage, unsigned empty) {
+  const long long base = blk * BLOCK, at = base + (VEC ? 4 * lane : lane);
+  const int live = VEC ? 8 : (int)min(max((T.n - at + 31) / 32, 0LL), 8LL);
+  auto offset = [](int j) { return VEC ? (j & 3) + (j >> 2) * 128 : 32 * j; };      // of the lane's j-th element
+  float p[8], g[8], m[8], v[8], r[8];
+  unsigned cm[2], cv[2];                           // the codes, four a word
+  if constexpr (VEC) {
+    const char *sp = stage + warp * BLOCK * 4, *sg = stage + CHUNK * 4 + warp * BLOCK * (T.g_type == NITI_F32 ? 4 : 2);
+    const char *sm = stage + CHUNK * 8 + warp * BLOCK * (EIGHT ? 1 : 4), *sv = sm + CHUNK * (EIGHT ? 1 : 4);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int i = 32 * h + lane;
+      *reinterpret_cast<float4 *>(p + 4 * h) = reinterpret_cast<const float4 *>(sp)[i];
+      if (EIGHT) {
+        cm[h] = reinterpret_cast<const unsigned *>(sm)[i];
+        cv[h] = reinterpret_cast<const unsigned *>(sv)[i];
+      } else {
+        *reinterpret_cast<float4 *>(m + 4 * h) = reinterpret_cast<const float4 *>(sm)[i];
+        *reinterpret_cast<float4 *>(v + 4 * h) = reinterpret_cast<const float4 *>(sv)[i];
+      }
+      if (T.g_type == NITI_F32) {
+        *reinterpret_cast<float4 *>(g + 4 * h) = reinterpret_cast<const float4 *>(sg)[i];
+      } else {
+        const uint2 w = reinterpret_cast<const uint2 *>(sg)[i];
+        if (T.g_type == NITI_BF16) {
+          g[4 * h] = __uint_as_float(w.x << 16); g[4 * h + 1] = __uint_as_float(w.x & 0xffff0000u);
+          g[4 * h + 2] = __uint_as_float(w.y << 16); g[4 * h + 3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+          const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&w.x)), b = __half22float2(*reinterpret_cast<const __half2 *>(&w.y));
+          g[4 * h] = a.x; g[4 * h + 1] = a.y; g[4 * h + 2] = b.x; g[4 * h + 3] = b.y;
+        }
+      }
+    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(empty);
+  } else {
+    cm[0] = cm[1] = cv[0] = cv[1] = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const long long e = at + offset(j);
+      const bool in = j < live;
+      p[j] = in ? T.p[e] : 0.0f;
+      g[j] = in ? load_grad(T.g, T.g_type, e) : 0.0f;
+      if (EIGHT) {
+        if (in) {
+          cm[j >> 2] |= (unsigned)((const uint8_t *)T.m)[e] << (8 * (j & 3));
+          cv[j >> 2] |= (unsigned)((const uint8_t *)T.v)[e] << (8 * (j & 3));
+        }
+      } else {
+        m[j] = in ? ((const float *)T.m)[e] : 0.0f;
+        v[j] = in ? ((const float *)T.v)[e] : 0.0f;
+      }
+    }
   }
-  const Tensor &T = l.t[lo];
-  const long long chunk = (long long)((int)blockIdx.x - l.first[lo]) * hy.blocks;
+  // the old states, already times b1 and b2
+  float k_m = st.b1, k_v = st.root_b2;
+  if (EIGHT) {
+    k_m *= niti_pow2(s_m);
+    k_v *= niti_pow2(s_v);
+    values_e4m3(cm[0], *reinterpret_cast<float (*)[4]>(m));
+    values_e4m3(cm[1], *reinterpret_cast<float (*)[4]>(m + 4));
+    values_e4m3(cv[0], *reinterpret_cast<float (*)[4]>(v));
+    values_e4m3(cv[1], *reinterpret_cast<float (*)[4]>(v + 4));
+  }
+  float worst = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) worst = niti_absmax(worst, g[j]);
+  const bool bad = !(worst * fabsf(st.gs) < __int_as_float(0x7f800000));
+  if (!bad) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] = fmaf(m[j], k_m, st.c1 * g[j]);
+      const float old = EIGHT ? (v[j] * k_v) * (v[j] * k_v) : v[j] * hy.b2;
+      v[j] = fmaf(st.c2 * g[j], g[j], old);
+      r[j] = root(v[j]);
+      p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
+    }
+  } else {                                         // (elements without a finite gradient keep what they have)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const bool ok = fabsf(g[j] * st.gs) < __int_as_float(0x7f800000);
+      const float old = EIGHT ? (v[j] * k_v) * (v[j] * k_v) : v[j] * hy.b2;
+      if (ok) {
+        m[j] = fmaf(m[j], k_m, st.c1 * g[j]);
+        v[j] = fmaf(st.c2 * g[j], g[j], old);
+      } else if (EIGHT) {
+        m[j] *= niti_pow2(s_m);
+        v[j] *= niti_pow2(s_v);
+        v[j] *= v[j];
+      }
+      r[j] = root(v[j]);
+      if (ok) p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
+    }
+  }
+  if (EIGHT) {
+    float am = 0.0f, ar = 0.0f, lm = fabsf(m[0]), lr = r[0];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      am = fmaxf(am, fabsf(m[j]));
+      ar = fmaxf(ar, r[j]);
+      lm = fminf(lm, fabsf(m[j]));
+      lr = fminf(lr, r[j]);
+    }
+    const int e_m = niti_exponent_of(__reduce_max_sync(0xffffffffu, __float_as_uint(am)), 8);
+    const int e_r = niti_exponent_of(__reduce_max_sync(0xffffffffu, __float_as_uint(ar)), 8);
+    const float q_m = niti_pow2(-e_m - 24), q_r = niti_pow2(-e_r - 24);
+    unsigned qm[8], qr[8];
+    // (few blocks hold a value below 2^-13 of their largest)
+    if (__any_sync(0xffffffffu, lm * q_m < LEAST_NORMAL || lr * q_r < LEAST_NORMAL)) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned x = random_bits((unsigned)at + (unsigned)offset(j), st.key);
+        qm[j] = draw_e4m3<true>(fabsf(m[j]) * q_m, x >> 16, st.sixteen);
+        // (at least the smallest code unless r is 0)
+        qr[j] = draw_e4m3<true>(r[j] > 0.0f ? fmaxf(r[j] * q_r, LEAST_CODE) : 0.0f, x & 0xffffu, st.sixteen);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const unsigned x = random_bits((unsigned)at + (unsigned)offset(j), st.key);
+        qm[j] = draw_e4m3<false>(fabsf(m[j]) * q_m, x >> 16, st.sixteen);
+        qr[j] = draw_e4m3<false>(r[j] * q_r, x & 0xffffu, st.sixteen);
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      unsigned s01, s23;                           // sign bytes of the moments
+      asm("prmt.b32 %0, %1, %2, 0x00fb;" : "=r"(s01) : "r"(__float_as_uint(m[4 * h])), "r"(__float_as_uint(m[4 * h + 1])));
+      asm("prmt.b32 %0, %1, %2, 0x00fb;" : "=r"(s23) : "r"(__float_as_uint(m[4 * h + 2])), "r"(__float_as_uint(m[4 * h + 3])));
+      cm[h] = pack_codes(qm[4 * h], qm[4 * h + 1], qm[4 * h + 2], qm[4 * h + 3]) | (__byte_perm(s01, s23, 0x5410) & 0x80808080u);
+      cv[h] = pack_codes(qr[4 * h], qr[4 * h + 1], qr[4 * h + 2], qr[4 * h + 3]);
+    }
+    s_m = e_m;
+    s_v = e_r;
+  }
+  if constexpr (VEC) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const long long e = at + 128 * h;
+      *reinterpret_cast<float4 *>(T.p + e) = *reinterpret_cast<float4 *>(p + 4 * h);
+      if (EIGHT) {
+        *reinterpret_cast<unsigned *>((uint8_t *)T.m + e) = cm[h];
+        *reinterpret_cast<unsigned *>((uint8_t *)T.v + e) = cv[h];
+      } else {
+        *reinterpret_cast<float4 *>((float *)T.m + e) = *reinterpret_cast<float4 *>(m + 4 * h);
+        *reinterpret_cast<float4 *>((float *)T.v + e) = *reinterpret_cast<float4 *>(v + 4 * h);
+      }
+      if (T.w8) *reinterpret_cast<unsigned *>(T.w8 + e) = niti_payload4<false>(p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3], st.w_scale);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= live) continue;
+      const long long e = at + offset(j);
+      T.p[e] = p[j];
+      if (EIGHT) {
+        ((uint8_t *)T.m)[e] = (uint8_t)(cm[j >> 2] >> (8 * (j & 3)));
+        ((uint8_t *)T.v)[e] = (uint8_t)(cv[j >> 2] >> (8 * (j & 3)));
+      } else {
+        ((float *)T.m)[e] = m[j];
+        ((float *)T.v)[e] = v[j];
+      }
+      if (T.w8) T.w8[e] = (int8_t)niti_payload<false>(p[j], st.w_scale);
+    }
+  }
+  return bad;
+}
+
+__device__ __forceinline__ void bulk_load(unsigned dst, const void *src, unsigned bytes, unsigned bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// Persistent: a CTA takes every n-th group of chunks, finds the step's constants once, and a warp of its own keeps the next
+// chunks' operands on their way into shared memory.  A group's block exponents are collected there, too, and stored by the warp
+// that comes last (32 bytes at once: one byte a warp and block took 60 us of 138 million weights' 418).
+template <int MOST, bool EIGHT>
+__global__ void __launch_bounds__(32 * WARPS + 32, ctas_per_sm(EIGHT))
+adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t *step, const float *grad_scale, uint32_t *status) {
+  extern __shared__ __align__(128) char smem[];
+  __shared__ __align__(8) unsigned long long bars[2 * STAGES];            // a stage is full, and has been read by all warps
+  __shared__ volatile int abort_flag;
+  // exponents of both states for four groups in turn: a warp that begins chunk k + STAGES + 1 waits until all have read chunk
+  // k + 1, and so are done with chunk k
+  __shared__ int8_t exps[STAGES + 1][2][GROUP * WARPS];
+  __shared__ int arrived[STAGES + 1];
+  if (threadIdx.x <= STAGES) arrived[threadIdx.x] = 0;
+  if (threadIdx.x < 2 * STAGES) {
+    mbar_init(smem_u32(&bars[threadIdx.x]), threadIdx.x < STAGES ? 1 : WARPS);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (threadIdx.x == 0) abort_flag = 0;
+  __syncthreads();
+  niti_enter(step, grad_scale);
+  const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = (int)threadIdx.x & 31;
   const int t_step = *step;
   if (t_step < 1) {                                // (1 - b^t would be no positive number)
     if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(status, NITI_DEV_BAD_STEP);
     return;
   }
-  const float fstep = (float)t_step, gs = grad_scale ? *grad_scale : 1.0f;
+  // (groups are dealt in turn, so that the grid works on neighbouring memory)
+  const int begin = (int)blockIdx.x, step_g = (int)gridDim.x, end = l.first[l.n], group = hy.group;
+  int lo = 0, hi = l.n;                            // the first group's tensor
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (l.first[mid] <= begin) lo = mid; else hi = mid;
+  }
+  // chunks of a group from element `first` on that are copied in bulk
+  auto bulk = [&](const Tensor &T, long long first) { return T.vec ? (int)min((T.n - first) / CHUNK, (long long)group) : 0; };
+  const unsigned smem0 = smem_u32(smem);
+  if (warp == WARPS) {                             // the copying warp (a copy takes its thread about 250 ns: not beside other work)
+    int stage = 0;
+    unsigned parity = 1u;
+    bool ok = true;
+    for (int gr = begin; lane == 0 && ok && gr < end; gr += step_g) {
+      while (gr >= l.first[lo + 1]) ++lo;
+      const Tensor &T = l.t[lo];
+      long long first = (long long)(gr - l.first[lo]) * group * CHUNK;
+      const unsigned gb = T.g_type == NITI_F32 ? 4 : 2, sb = EIGHT ? 1 : 4;
+      for (int left = bulk(T, first); left > 0; --left, first += CHUNK) {
+        if (!mbar_wait(smem_u32(&bars[STAGES + stage]), parity, &abort_flag, status)) { ok = false; break; }
+        const unsigned bar = smem_u32(&bars[stage]), dst = smem0 + stage * stage_bytes(EIGHT);
+        mbar_expect_tx(bar, CHUNK * (4 + gb + 2 * sb));
+        bulk_load(dst, T.p + first, CHUNK * 4, bar);
+        bulk_load(dst + CHUNK * 4, (const char *)T.g + first * gb, CHUNK * gb, bar);
+        bulk_load(dst + CHUNK * 8, (const char *)T.m + first * sb, CHUNK * sb, bar);
+        bulk_load(dst + CHUNK * (8 + sb), (const char *)T.v + first * sb, CHUNK * sb, bar);
+        if (++stage == STAGES) { stage = 0; parity ^= 1u; }
+      }
+    }
+    __syncwarp();
+    if (abort_flag) {                              // copies in flight land before the shared memory goes away
+      const long long t0 = clock64();
+      while (clock64() - t0 < 20000000LL) {
+      }
+    }
+    return;
+  }
+  Step st;
   // 1 - b^t without its cancellation
-  const float lr_m = hy.lr / -expm1f(fstep * hy.log_b1), rs_v = rsqrtf(-expm1f(fstep * hy.log_b2));
-  const float decay = T.decay;
-  const bool with_w8 = T.w8 != nullptr;
-  const int s_w = with_w8 ? *T.s_w : 0;
-  const float w_scale = niti_pow2(s_w < -126 ? 126 : s_w > 126 ? -126 : -s_w);
-  const unsigned key = (unsigned)t_step * 0x9E3779B9u;
+  const float lr = fmaxf(hy.lr / -expm1f((float)t_step * hy.log_b1), 1e-37f);        // (0: a step of nothing)
+  st.den_r = -rsqrtf(-expm1f((float)t_step * hy.log_b2)) / lr;
+  st.den_1 = -hy.eps / lr;
+  st.gs = grad_scale ? *grad_scale : 1.0f;
+  st.b1 = hy.b1;
+  st.root_b2 = hy.root_b2;
+  st.c1 = hy.c1 * st.gs;
+  st.c2 = hy.c2 * st.gs * st.gs;
+  st.key = (unsigned)t_step * 0x9E3779B9u;
+  st.sixteen = 16u;
+  asm volatile("" : "+r"(st.sixteen));
   bool bad = false;
-  for (int i = warp; i < hy.blocks; i += WARPS) {
-    const long long blk = chunk + i, base = blk * BLOCK;
-    if (base >= T.n) break;
-    const bool vec = T.vec && base + BLOCK <= T.n;
-    const long long at = base + (vec ? lane * 8 : lane);
-    const int stride = vec ? 1 : 32;
-    const int live = vec ? 8 : (int)((T.n - at + 31) / 32 < 0 ? 0 : (T.n - at + 31) / 32 > 8 ? 8 : (T.n - at + 31) / 32);
-    float p[8], g[8], m[8], v[8];
-    unsigned cm[8], cv[8];
-    if (vec) {
-      *reinterpret_cast<float4 *>(p) = __ldcs(reinterpret_cast<const float4 *>(T.p + at));
-      *reinterpret_cast<float4 *>(p + 4) = __ldcs(reinterpret_cast<const float4 *>(T.p + at) + 1);
-      if (T.g_type == NITI_F32) {
-        *reinterpret_cast<float4 *>(g) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.g + at));
-        *reinterpret_cast<float4 *>(g + 4) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.g + at) + 1);
-      } else if (T.g_type == NITI_BF16) {
-        Pack<NITI_BF16, 8> k;
-        k.load(T.g, at);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = k.get(j);
-      } else {
-        Pack<NITI_F16, 8> k;
-        k.load(T.g, at);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) g[j] = k.get(j);
-      }
+  int stage = 0;
+  unsigned parity = 0;
+  int next_m = 0, next_v = 0;                      // exponents of the warp's block of chunk `ready` of tensor `known`
+  long long ready = -1;
+  bool ok = true;
+  for (int gr = begin, known = -1, turn = 0; ok && gr < end; gr += step_g, turn = turn == STAGES ? 0 : turn + 1) {
+    while (gr >= l.first[lo + 1]) ++lo;
+    const Tensor &T = l.t[lo];
+    if (lo != known) {
+      known = lo;
+      ready = -1;
+      const int s_w = T.w8 ? *T.s_w : 0;
+      st.w_scale = niti_pow2(s_w < -126 ? 126 : s_w > 126 ? -126 : -s_w);
+      st.decay = T.decay;
+    }
+    const long long chunk0 = (long long)(gr - l.first[lo]) * group;
+    const int whole = bulk(T, chunk0 * CHUNK);
+    for (int j = 0; j < group; ++j) {
+      const long long chunk = chunk0 + j, blk = chunk * WARPS + warp;
+      if (chunk * CHUNK >= T.n) break;
+      int s_m = next_m, s_v = next_v;
       if (EIGHT) {
-        const uint2 a = __ldcs(reinterpret_cast<const uint2 *>((const uint8_t *)T.m + at));
-        const uint2 b = __ldcs(reinterpret_cast<const uint2 *>((const uint8_t *)T.v + at));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          cm[j] = ((j < 4 ? a.x : a.y) >> (8 * (j & 3))) & 255u;
-          cv[j] = ((j < 4 ? b.x : b.y) >> (8 * (j & 3))) & 255u;
+        if (ready != chunk && blk * BLOCK < T.n) {
+          s_m = T.s_m[blk];
+          s_v = T.s_v[blk];
         }
-      } else {
-        *reinterpret_cast<float4 *>(m) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.m + at));
-        *reinterpret_cast<float4 *>(m + 4) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.m + at) + 1);
-        *reinterpret_cast<float4 *>(v) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.v + at));
-        *reinterpret_cast<float4 *>(v + 4) = __ldcs(reinterpret_cast<const float4 *>((const float *)T.v + at) + 1);
+        ready = j + 1 < group ? chunk + 1 : chunk + 1 + (long long)(step_g - 1) * group;
+        const long long next = ready * WARPS + warp;
+        if (next * BLOCK < T.n) {
+          next_m = T.s_m[next];
+          next_v = T.s_v[next];
+        }
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const long long e = at + j * stride;
-        const bool in = j < live;
-        p[j] = in ? T.p[e] : 0.0f;
-        g[j] = in ? load_grad(T.g, T.g_type, e) : 0.0f;
+      if (j < whole) {
+        if (!mbar_wait_warp(smem_u32(&bars[stage]), parity, &abort_flag, status)) { ok = false; break; }
+        bad |= adamw_block<EIGHT, true>(T, hy, st, blk, warp, lane, s_m, s_v, smem + stage * stage_bytes(EIGHT), smem_u32(&bars[STAGES + stage]));
+        if (++stage == STAGES) { stage = 0; parity ^= 1u; }
         if (EIGHT) {
-          cm[j] = in ? ((const uint8_t *)T.m)[e] : 0u;
-          cv[j] = in ? ((const uint8_t *)T.v)[e] : 0u;
-        } else {
-          m[j] = in ? ((const float *)T.m)[e] : 0.0f;
-          v[j] = in ? ((const float *)T.v)[e] : 0.0f;
+          int before = 0;
+          if (lane == 0) {
+            exps[turn][0][j * WARPS + warp] = (int8_t)s_m;
+            exps[turn][1][j * WARPS + warp] = (int8_t)s_v;
+            __threadfence_block();
+            before = atomicAdd(&arrived[turn], 1);
+          }
+          if (__shfl_sync(0xffffffffu, before, 0) == whole * WARPS - 1) {
+            __threadfence_block();
+            if (lane < whole * WARPS) {
+              T.s_m[chunk0 * WARPS + lane] = *(volatile int8_t *)&exps[turn][0][lane];
+              T.s_v[chunk0 * WARPS + lane] = *(volatile int8_t *)&exps[turn][1][lane];
+            }
+            if (lane == 0) arrived[turn] = 0;
+            __threadfence_block();
+          }
+        }
+      } else if (blk * BLOCK < T.n) {
+        bad |= adamw_block<EIGHT, false>(T, hy, st, blk, warp, lane, s_m, s_v, nullptr, 0u);
+        if (EIGHT && lane == 0) {
+          T.s_m[blk] = (int8_t)s_m;
+          T.s_v[blk] = (int8_t)s_v;
         }
       }
     }
-    if (EIGHT) {
-      const float k_m = niti_pow2((int)T.s_m[blk]), k_v = niti_pow2((int)T.s_v[blk]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float mm = value_e4m3(cm[j] & 127u) * k_m, r = value_e4m3(cv[j] & 127u) * k_v;
-        m[j] = (cm[j] & 128u) ? -mm : mm;
-        v[j] = r * r;
-      }
-    }
-    float r[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gj = g[j] * gs;
-      const bool ok = fabsf(gj) < __int_as_float(0x7f800000);
-      if (ok) {
-        m[j] = fmaf(hy.b1, m[j], hy.c1 * gj);
-        v[j] = fmaf(hy.b2, v[j], hy.c2 * gj * gj);
-      }
-      r[j] = root(v[j]);
-      if (ok) p[j] = fmaf(p[j], decay, -lr_m * __fdividef(m[j], fmaf(r[j], rs_v, hy.eps)));
-      bad |= !ok;
-    }
-    if (EIGHT) {
-      unsigned am = 0, ar = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        am = max(am, __float_as_uint(m[j]) & 0x7fffffffu);
-        ar = max(ar, __float_as_uint(r[j]));
-      }
-      const int e_m = niti_exponent_of(__reduce_max_sync(0xffffffffu, am), 8), e_r = niti_exponent_of(__reduce_max_sync(0xffffffffu, ar), 8);
-      const float k_m = niti_pow2(-e_m), k_r = niti_pow2(-e_r);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        unsigned fm, fr;
-        split_e4m3(fabsf(m[j]) * k_m, cm[j], fm);
-        split_e4m3(r[j] * k_r, cv[j], fr);
-        const unsigned x = random_bits((unsigned)(at + j * stride), key);
-        cm[j] += (fm + (x >> 16)) >> 16;
-        cv[j] += (fr + (x & 0xffffu)) >> 16;
-        if (cv[j] == 0u && r[j] > 0.0f) cv[j] = 1u;
-        if (m[j] < 0.0f) cm[j] |= 128u;
-      }
-      if (lane == 0) {
-        T.s_m[blk] = (int8_t)e_m;
-        T.s_v[blk] = (int8_t)e_r;
-      }
-    }
-    if (vec) {
-      reinterpret_cast<float4 *>(T.p + at)[0] = *reinterpret_cast<float4 *>(p);
-      reinterpret_cast<float4 *>(T.p + at)[1] = *reinterpret_cast<float4 *>(p + 4);
-      if (EIGHT) {
-        *reinterpret_cast<uint2 *>((uint8_t *)T.m + at) =
-            make_uint2(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24);
-        *reinterpret_cast<uint2 *>((uint8_t *)T.v + at) =
-            make_uint2(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24, cv[4] | cv[5] << 8 | cv[6] << 16 | cv[7] << 24);
-      } else {
-        reinterpret_cast<float4 *>((float *)T.m + at)[0] = *reinterpret_cast<float4 *>(m);
-        reinterpret_cast<float4 *>((float *)T.m + at)[1] = *reinterpret_cast<float4 *>(m + 4);
-        reinterpret_cast<float4 *>((float *)T.v + at)[0] = *reinterpret_cast<float4 *>(v);
-        reinterpret_cast<float4 *>((float *)T.v + at)[1] = *reinterpret_cast<float4 *>(v + 4);
-      }
-      if (with_w8) {
-        int q[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = niti_payload(p[j], w_scale, NITI_ROUND_NEAREST);
-        niti_store_payload<8>(T.w8, at, q);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (j >= live) continue;
-        const long long e = at + j * stride;
-        T.p[e] = p[j];
-        if (EIGHT) {
-          ((uint8_t *)T.m)[e] = (uint8_t)cm[j];
-          ((uint8_t *)T.v)[e] = (uint8_t)cv[j];
-        } else {
-          ((float *)T.m)[e] = m[j];
-          ((float *)T.v)[e] = v[j];
-        }
-        if (with_w8) T.w8[e] = (int8_t)niti_payload(p[j], w_scale, NITI_ROUND_NEAREST);
-      }
+  }
+  if (abort_flag) {                                // (as above)
+    const long long t0 = clock64();
+    while (clock64() - t0 < 20000000LL) {
     }
   }
   if (__any_sync(0xffffffffu, bad) && lane == 0) atomicOr(status, NITI_DEV_NONFINITE);
 }
 
 template <int MOST>
-int launch(niti_ctx *ctx, cudaStream_t st, const niti_adamw_tensor *t, int n, bool eight, const Hyper &hyper, double lr, const int32_t *step,
+int launch(niti_ctx *ctx, cudaStream_t st, const niti_adamw_tensor *t, int n, bool eight, Hyper hy, double lr, const int32_t *step,
            const float *grad_scale) {
   List<MOST> l;
-  Hyper hy = hyper;
-  long long total = 0;
-  for (int i = 0; i < n; ++i) total += (t[i].n + BLOCK - 1) / BLOCK;
-  // a chunk of several blocks a warp shares the set-up between them; with few blocks every warp has one
-  hy.blocks = total >= 16LL * WARPS * ctx->sm_count ? 4 * WARPS : WARPS;
-  long long chunks = 0;
+  long long chunks = 0, groups = 0;
+  for (int i = 0; i < n; ++i) chunks += (t[i].n + CHUNK - 1) / CHUNK;
+  const long long most = (long long)ctx->sm_count * ctas_per_sm(eight);
+  hy.group = chunks >= 4 * GROUP * most ? GROUP : 1;           // (few chunks: one for every CTA)
   l.n = n;
   for (int i = 0; i < n; ++i) {
     const niti_adamw_tensor &a = t[i];
@@ -262,19 +454,28 @@ int launch(niti_ctx *ctx, cudaStream_t st, const niti_adamw_tensor *t, int n, bo
     b.n = a.n;
     b.decay = (float)(1.0 - lr * (double)a.weight_decay);
     b.g_type = (short)a.g_type;
-    const uintptr_t wide = (uintptr_t)a.p | (uintptr_t)a.g | (eight ? 0 : (uintptr_t)a.m | (uintptr_t)a.v);
-    const uintptr_t narrow = (uintptr_t)a.w8 | (eight ? (uintptr_t)a.m | (uintptr_t)a.v : 0);
-    b.vec = (wide & 15) == 0 && (narrow & 7) == 0;
-    l.first[i] = (int)chunks;
-    chunks += ((a.n + BLOCK - 1) / BLOCK + hy.blocks - 1) / hy.blocks;
-    if (chunks >= (1LL << 31)) return niti_fail(ctx, NITI_ERR_SHAPE, "niti_adamw: too many elements in one list");
+    b.vec = (((uintptr_t)a.p | (uintptr_t)a.g | (uintptr_t)a.m | (uintptr_t)a.v) & 15) == 0 && ((uintptr_t)a.w8 & 3) == 0;
+    l.first[i] = (int)groups;
+    groups += (a.n + (long long)CHUNK * hy.group - 1) / ((long long)CHUNK * hy.group);
+    if (groups >= (1LL << 30)) return niti_fail(ctx, NITI_ERR_SHAPE, "niti_adamw: too many elements in one list");
   }
-  for (int i = n; i <= MOST; ++i) l.first[i] = (int)chunks;
-  if (!chunks) return NITI_OK;
-  if (eight)
-    NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)chunks, 32 * WARPS, 0, adamw_kernel<MOST, true>, l, hy, step, grad_scale, ctx->d_status));
-  else
-    NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)chunks, 32 * WARPS, 0, adamw_kernel<MOST, false>, l, hy, step, grad_scale, ctx->d_status));
+  for (int i = n; i <= MOST; ++i) l.first[i] = (int)groups;
+  if (!groups) return NITI_OK;
+  const unsigned grid = (unsigned)(groups < most ? groups : most);
+  auto go = [&](auto kernel) -> int {
+    // (the device's limit, as for every kernel of the library: see niti_ctx::smem_optin)
+    bool &ready = ctx->adamw_ready[(MOST == LIST_MOST ? 2 : 0) + (eight ? 1 : 0)];
+    if (!ready) {
+      cudaFuncAttributes fa;
+      NITI_CUDA_TRY(ctx, cudaFuncGetAttributes(&fa, kernel));
+      NITI_CUDA_TRY(ctx, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(ctx->smem_optin - fa.sharedSizeBytes)));
+      ready = true;
+    }
+    NITI_CUDA_TRY(ctx, niti_launch(st, grid, 32 * WARPS + 32, (size_t)STAGES * stage_bytes(eight), kernel, l, hy, step, grad_scale, ctx->d_status));
+    return NITI_OK;
+  };
+  const int rc = eight ? go(adamw_kernel<MOST, true>) : go(adamw_kernel<MOST, false>);
+  if (rc != NITI_OK) return rc;
   ctx->launches++;
   return NITI_OK;
 }
@@ -303,6 +504,7 @@ extern "C" int niti_adamw(niti_ctx *ctx, void *stream, const niti_adamw_tensor *
   hy.lr = (float)lr;
   hy.b1 = (float)beta1; hy.b2 = (float)beta2;
   hy.c1 = (float)(1.0 - beta1); hy.c2 = (float)(1.0 - beta2);
+  hy.root_b2 = (float)sqrt(beta2);
   hy.eps = (float)eps;
   // (b = 0: 1 - b^t is 1 for every t >= 1)
   hy.log_b1 = beta1 > 0.0 ? (float)log(beta1) : -1e30f;

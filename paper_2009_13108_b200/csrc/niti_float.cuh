@@ -38,6 +38,21 @@ struct Pack {
     else if constexpr (BYTES == 4) *reinterpret_cast<unsigned *>(q) = w[0];
     else *reinterpret_cast<unsigned short *>(q) = (unsigned short)w[0];
   }
+  // this + b, rounded to the type once
+  __device__ __forceinline__ void add(const Pack &b) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (T == NITI_F32) {
+        w[i] = __float_as_uint(__uint_as_float(w[i]) + __uint_as_float(b.w[i]));
+      } else if constexpr (T == NITI_BF16) {
+        const __nv_bfloat162 s = __hadd2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i]), *reinterpret_cast<const __nv_bfloat162 *>(&b.w[i]));
+        w[i] = *reinterpret_cast<const unsigned *>(&s);
+      } else {
+        const __half2 s = __hadd2(*reinterpret_cast<const __half2 *>(&w[i]), *reinterpret_cast<const __half2 *>(&b.w[i]));
+        w[i] = *reinterpret_cast<const unsigned *>(&s);
+      }
+    }
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) w[i] = 0u;
@@ -121,38 +136,58 @@ __device__ __forceinline__ int niti_exponent_of(unsigned max_bits, int integer_b
 // 2^e for e in [-126, 127]
 __device__ __forceinline__ float niti_pow2(int e) { return __int_as_float((e + 127) << 23); }
 
-// Magnitude u in units of the result to a whole number, at most 127.  Pseudo-stochastic: the 16 fraction bits are split
-// into halves, rounded up where the top half is larger than the bottom half (Algorithm 3 with bp = 16; the sum carries
-// into bit 16 exactly then).  To nearest: half up, as everywhere in the library.  (Conversions saturate, and turn NaN
-// into 0.)
-__device__ __forceinline__ int niti_round_units(float u, int round_mode) {
-  unsigned q;
-  if (round_mode == NITI_ROUND_PSR) {
-    const unsigned v = __float2uint_rz(u * 65536.0f);
-    q = v >= (127u << 16) ? 127u : (v + ((~v & 255u) << 8)) >> 16;
-  } else {
-    q = __float2uint_rz(u + 0.5f);
-  }
-  return (int)(q > 127u ? 127u : q);
-}
-// scale = 2^-s (times whatever else scales the tensor)
-__device__ __forceinline__ int niti_payload(float x, float scale, int round_mode) {
-  const int q = niti_round_units(fabsf(x) * scale, round_mode);
-  return x < 0.0f ? -q : q;
+// The larger magnitude of two, NaN if either is.
+__device__ __forceinline__ float niti_absmax(float m, float x) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(m), "f"(fabsf(x)));
+  return r;
 }
 
-// VEC payload bytes at p + i
-template <int VEC>
-__device__ __forceinline__ void niti_store_payload(int8_t *p, long long i, const int (&q)[VEC]) {
-  if constexpr (VEC == 1) {
-    p[i] = (int8_t)q[0];
+// Magnitudes in units of the result to whole numbers, at most 127.  Pseudo-stochastic: the 16 fraction bits are split into
+// halves, rounded up where the top half is larger than the bottom half (Algorithm 3 with bp = 16; the sum carries into bit
+// 16 exactly then).  To nearest: half up, as everywhere in the library.  (Conversions saturate, and turn NaN into 0.)
+// `scale` is that of niti_payload_scale(): in the first case results come in bits 16 .. 22, so that the multiplication
+// that scales also makes room for the fraction.
+__device__ __forceinline__ float niti_payload_scale(float units, int round_mode) {
+  return round_mode == NITI_ROUND_PSR ? units * 65536.0f : units;
+}
+template <bool PSR>
+__device__ __forceinline__ unsigned niti_unit_mag(float x, float scale) {
+  if constexpr (PSR) {
+    const unsigned v = min(__float2uint_rz(fabsf(x) * scale), 127u << 16);
+    return v + (~v & 255u) * 256u;
   } else {
-    unsigned w[VEC / 4];
-#pragma unroll
-    for (int j = 0; j < VEC / 4; ++j)
-      w[j] = (unsigned)(q[4 * j] & 255) | (unsigned)(q[4 * j + 1] & 255) << 8 | (unsigned)(q[4 * j + 2] & 255) << 16 |
-             (unsigned)q[4 * j + 3] << 24;
-    if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(p + i) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<unsigned *>(p + i) = w[0];
+    return min(__float2uint_rz(fmaf(fabsf(x), scale, 0.5f)), 127u);
+  }
+}
+// (of 127 << 16 the sum is 127 << 16 | 0xff00: the same byte)
+template <bool PSR>
+__device__ __forceinline__ int niti_payload(float x, float scale) {
+  const int q = (int)(PSR ? niti_unit_mag<PSR>(x, scale) >> 16 : niti_unit_mag<PSR>(x, scale));
+  return x < 0.0f ? -q : q;
+}
+// Four payloads in a word: magnitudes gathered by byte permutes, signs as bytes of zeros or ones (a permute with sign
+// replication), and two's complement of four bytes at once: the low seven bits plus one where negative do not reach the next
+// byte, and their carry into bit 7 turns the sign off again for a magnitude of zero.  7.5 instructions a value, 13 one by one.
+template <bool PSR>
+__device__ __forceinline__ unsigned niti_payload4(float x0, float x1, float x2, float x3, float scale) {
+  const unsigned a = niti_unit_mag<PSR>(x0, scale), b = niti_unit_mag<PSR>(x1, scale), c = niti_unit_mag<PSR>(x2, scale), d = niti_unit_mag<PSR>(x3, scale);
+  constexpr unsigned PAIR = PSR ? 0x0062u : 0x0040u;                       // byte 2 (0) of both
+  const unsigned m = __byte_perm(__byte_perm(a, b, PAIR), __byte_perm(c, d, PAIR), 0x5410);
+  unsigned s01, s23, s;
+  asm("prmt.b32 %0, %1, %2, 0x00fb;" : "=r"(s01) : "r"(__float_as_uint(x0)), "r"(__float_as_uint(x1)));    // sign bytes of both
+  asm("prmt.b32 %0, %1, %2, 0x00fb;" : "=r"(s23) : "r"(__float_as_uint(x2)), "r"(__float_as_uint(x3)));
+  s = __byte_perm(s01, s23, 0x5410);
+  return (((m ^ s) & 0x7f7f7f7fu) + (s & 0x01010101u)) ^ (s & 0x80808080u);
+}
+// VEC payload bytes at p + i
+template <int VEC, bool PSR>
+__device__ __forceinline__ void niti_store_payload(int8_t *p, long long i, const float (&x)[VEC], float scale) {
+  if constexpr (VEC == 1) {
+    p[i] = (int8_t)niti_payload<PSR>(x[0], scale);
+  } else {
+    const unsigned w0 = niti_payload4<PSR>(x[0], x[1], x[2], x[3], scale);
+    if constexpr (VEC == 8) *reinterpret_cast<uint2 *>(p + i) = make_uint2(w0, niti_payload4<PSR>(x[4], x[5], x[6], x[7], scale));
+    else *reinterpret_cast<unsigned *>(p + i) = w0;
   }
 }

@@ -594,7 +594,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
   const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = (int)blockIdx.y * rows, r1 = min(r0 + rows, M);
   if (next && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) niti_zero_header(next, (int)threadIdx.x);
   float sum[VEC];
-  unsigned most = 0;
+  float largest = 0.0f;
 #pragma unroll
   for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
   if (c < N) {
@@ -602,7 +602,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         sum[j] += e[j];
-        most = max(most, __float_as_uint(e[j]) & 0x7fffffffu);
+        largest = niti_absmax(largest, e[j]);
       }
     });
     if (part) {
@@ -610,19 +610,19 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
       for (int j = 0; j < VEC; ++j) part[(long long)blockIdx.y * N + c + j] = sum[j];
     }
   }
-  most = __reduce_max_sync(0xffffffffu, most);
+  const unsigned most = __reduce_max_sync(0xffffffffu, __float_as_uint(largest));
   if ((threadIdx.x & 31) == 0 && most) atomicMax(&hdr->maxabs32, most);
 }
 
 // e as payload with the exponent of its maximum, rows of `pitch` bytes.  The rows that the pass before read last come first.
-template <int T, int VEC, int ACT>
+template <int T, int VEC, int ACT, bool PSR>
 __global__ void __launch_bounds__(ERR_THREADS)
 error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, int rows,
-                   int pitch, int round_mode) {
+                   int pitch) {
   niti_enter(dout, z, hdr);
   const unsigned most = hdr->maxabs32;
   const int s = niti_exponent_of(most);
-  const float scale = niti_pow2(-s);
+  const float scale = niti_payload_scale(niti_pow2(-s), PSR ? NITI_ROUND_PSR : NITI_ROUND_NEAREST);
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
     *s_e = s;
     if (most >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
@@ -631,10 +631,7 @@ error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, co
   const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * rows, r1 = min(r0 + rows, M);
   if (c >= N) return;
   error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
-    int q[VEC];
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) q[j] = niti_payload(e[j], scale, round_mode);
-    niti_store_payload<VEC>(e8, (long long)r * pitch + c, q);
+    niti_store_payload<VEC, PSR>(e8, (long long)r * pitch + c, e, scale);
   });
 }
 
@@ -748,10 +745,16 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
     ctx->launches++;
     niti_header_passed_on(ctx, next);
     if (!dx && !dw) return NITI_OK;
-    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT>, dout, z, e8, s_e, (const WsHeader *)hdr, ctx->d_status, M,
-                                   N, rows, pitch_e, round_mode));
-    ctx->launches++;
-    return NITI_OK;
+    auto second = [&](auto psr) -> int {
+      NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT, decltype(psr)::value>, dout, z, e8, s_e,
+                                     (const WsHeader *)hdr, ctx->d_status, M, N, rows, pitch_e));
+      ctx->launches++;
+      return NITI_OK;
+    };
+    // (16-bit types without an activation or with a ReLU are not rounded pseudo-stochastically)
+    if constexpr (T == NITI_F32 || ACT == NITI_ACT_GELU || ACT == NITI_ACT_SILU)
+      if (round_mode == NITI_ROUND_PSR) return second(std::true_type{});
+    return second(std::false_type{});
   };
   auto passes = [&](auto tc, auto vc) -> int {
     switch (act) {

@@ -34,11 +34,28 @@ __device__ __forceinline__ void row_reduce(float &ss, unsigned &am, int tpr, int
   am = __reduce_max_sync(0xffffffffu, __float_as_uint(v.y));
 }
 
+// Rounding of a launch: a template parameter where a thread has vectors, looked up where it has single elements.
+enum { ROUND_BY_ARGUMENT = 2 };
+template <int VEC, int MODE>
+__device__ __forceinline__ void store_payload(int8_t *y, long long at, const float (&x)[VEC], float scale, int round_mode) {
+  if constexpr (MODE == ROUND_BY_ARGUMENT) {
+    if (round_mode == NITI_ROUND_PSR) niti_store_payload<VEC, true>(y, at, x, scale);
+    else niti_store_payload<VEC, false>(y, at, x, scale);
+  } else {
+    niti_store_payload<VEC, MODE == NITI_ROUND_PSR>(y, at, x, scale);
+  }
+}
+// The bits of the largest magnitude of a row, INF_BITS or more where something is not finite: a value, or the squares' sum
+// (then r is 0 or NaN, and nothing of the row means anything).
+__device__ __forceinline__ unsigned row_top(unsigned am, float ss, float r) {
+  return am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
+}
+
 // y = h r gain with h = x + residual, r = 1 / sqrt(mean(h^2) + eps); without NORM y = x.  A thread holds NV vectors of its
 // row, and the next row's are on their way while this one's sums are taken.  The maximum that fixes the exponent is taken
 // of |h gain| beside the sum of squares, since r only scales it: one reduction a row.
 // SHARED: only h, r and the maximum over the tensor; norm_round_kernel follows.
-template <int T, int VEC, int NV, bool NORM, bool SHARED>
+template <int T, int VEC, int NV, bool NORM, bool SHARED, int MODE>
 __global__ void __launch_bounds__(ROW_MOST)
 norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int8_t *y, int32_t *s_y, float *rstd,
                  WsHeader *hdr, WsHeader *next, uint32_t *status, RowShape sh, float eps, int round_mode) {
@@ -71,39 +88,36 @@ norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int
   int row = (int)blockIdx.x * sh.rpb + grp;
   fetch(row);
   unsigned most = 0;
+  const float inv_c = 1.0f / (float)sh.C;
   for (int turn = 0, base = (int)blockIdx.x * sh.rpb; base < sh.M; base += step, row += step, turn ^= 1) {
     const bool rok = row < sh.M;
     const long long at = (long long)row * sh.C + t * VEC;
     float hv[NV][VEC];
-    float ss = 0.0f;
-    unsigned am = 0;
+    float ss = 0.0f, am = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
+      if (NORM && res) {                               // (the norm is that of the stored row)
+        px[v].add(pr[v]);
+        if (in[v] && rok) px[v].store(h, at + (long long)v * sh.tpr * VEC);
+      }
 #pragma unroll
       for (int j = 0; j < VEC; ++j) hv[v][j] = px[v].get(j);
-      if (NORM && res) {
-        Pack<T, VEC> ph;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) hv[v][j] += pr[v].get(j);
-        ph.set(hv[v]);
-        if (in[v] && rok) ph.store(h, at + (long long)v * sh.tpr * VEC);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) hv[v][j] = ph.get(j);         // (the norm is that of the stored row)
-      }
     }
     fetch(row + step < sh.M ? row + step : sh.M);
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
-        if (NORM) ss = fmaf(hv[v][j], hv[v][j], ss);
-        hv[v][j] *= g[v][j];
-        if (in[v]) am = max(am, __float_as_uint(hv[v][j]) & 0x7fffffffu);
+        if (NORM) {
+          ss = fmaf(hv[v][j], hv[v][j], ss);
+          hv[v][j] *= g[v][j];
+        }
+        am = niti_absmax(am, in[v] ? hv[v][j] : 0.0f);
       }
-    row_reduce(ss, am, sh.tpr, warp, lane, buf, turn);
-    const float r = NORM ? rsqrtf(ss / (float)sh.C + eps) : 1.0f;
-    // (r is 0 or NaN where the squares left the float range, and then nothing of the row means anything)
-    const unsigned top = am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
+    unsigned ab = __float_as_uint(am);
+    row_reduce(ss, ab, sh.tpr, warp, lane, buf, turn);
+    const float r = NORM ? rsqrtf(fmaf(ss, inv_c, eps)) : 1.0f;
+    const unsigned top = row_top(ab, ss, r);
     if (t == 0 && rok) {
       if (top >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
       if (NORM && rstd) rstd[row] = r;
@@ -113,15 +127,11 @@ norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int
       continue;
     }
     const int s = niti_exponent_of(top);
-    const float scale = r * niti_pow2(-s);
+    const float scale = niti_payload_scale(r * niti_pow2(-s), round_mode);
     if (t == 0 && rok) s_y[row] = s;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      int q[VEC];
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) q[j] = niti_payload(hv[v][j], scale, round_mode);
-      if (in[v] && rok) niti_store_payload<VEC>(y, at + (long long)v * sh.tpr * VEC, q);
-    }
+    for (int v = 0; v < NV; ++v)
+      if (in[v] && rok) store_payload<VEC, MODE>(y, at + (long long)v * sh.tpr * VEC, hv[v], scale, round_mode);
   }
   if (SHARED) {
     most = __reduce_max_sync(0xffffffffu, most);
@@ -131,7 +141,7 @@ norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int
 
 // Payload of a whole tensor with the exponent of its maximum, from h (or x) and r.  The rows that norm_rows_kernel read
 // last come first: they are still in L2.
-template <int T, int VEC, bool NORM>
+template <int T, int VEC, bool NORM, int MODE>
 __global__ void __launch_bounds__(ROW_THREADS)
 norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y, int32_t *s_y, const WsHeader *hdr, int M, int C,
                   int parts, int round_mode) {
@@ -144,13 +154,13 @@ norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y
     const int row = M - 1 - (int)(it / parts), part = (int)(it % parts);
     const int c = (part * ROW_THREADS + (int)threadIdx.x) * VEC;
     if (c >= C) continue;
-    const float scale = NORM ? rstd[row] * p2 : p2;
+    const float scale = niti_payload_scale(NORM ? rstd[row] * p2 : p2, round_mode);
     Pack<T, VEC> p;
     p.load(h, (long long)row * C + c);
-    int q[VEC];
+    float v[VEC];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) q[j] = niti_payload(NORM ? p.get(j) * gain[c + j] : p.get(j), scale, round_mode);
-    niti_store_payload<VEC>(y, (long long)row * C + c, q);
+    for (int j = 0; j < VEC; ++j) v[j] = NORM ? p.get(j) * gain[c + j] : p.get(j);
+    store_payload<VEC, MODE>(y, (long long)row * C + c, v, scale, round_mode);
   }
 }
 
@@ -167,26 +177,24 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
   int turn = 0;
   for (int row = (int)blockIdx.x; row < M; row += (int)gridDim.x, turn ^= 1) {
     const long long at = (long long)row * C;
-    float ss = 0.0f;
-    unsigned am = 0;
+    float ss = 0.0f, am = 0.0f;
     for (int c = (int)threadIdx.x; c < C; c += 1024) {
       Pack<T, 1> p;
       p.load(x, at + c);
-      float v = p.get(0);
       if (NORM && res) {
         Pack<T, 1> pr;
         pr.load(res, at + c);
-        const float sum[1] = {v + pr.get(0)};
-        p.set(sum);
+        p.add(pr);
         p.store(h, at + c);
-        v = p.get(0);
       }
+      const float v = p.get(0);
       if (NORM) ss = fmaf(v, v, ss);
-      am = max(am, __float_as_uint(NORM ? v * gain[c] : v) & 0x7fffffffu);
+      am = niti_absmax(am, NORM ? v * gain[c] : v);
     }
-    row_reduce(ss, am, 1024, warp, lane, buf, turn);
+    unsigned ab = __float_as_uint(am);
+    row_reduce(ss, ab, 1024, warp, lane, buf, turn);
     const float r = NORM ? rsqrtf(ss / (float)C + eps) : 1.0f;
-    const unsigned top = am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
+    const unsigned top = row_top(ab, ss, r);
     if (threadIdx.x == 0) {
       if (top >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
       if (NORM && rstd) rstd[row] = r;
@@ -196,13 +204,14 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
       continue;
     }
     const int s = niti_exponent_of(top);
-    const float scale = r * niti_pow2(-s);
+    const float scale = niti_payload_scale(r * niti_pow2(-s), round_mode);
     if (threadIdx.x == 0) s_y[row] = s;
     const void *src = NORM && res ? h : x;            // (each thread reads what it has written itself)
     for (int c = (int)threadIdx.x; c < C; c += 1024) {
       Pack<T, 1> p;
       p.load(src, at + c);
-      y[at + c] = (int8_t)niti_payload(NORM ? p.get(0) * gain[c] : p.get(0), scale, round_mode);
+      const float v[1] = {NORM ? p.get(0) * gain[c] : p.get(0)};
+      store_payload<1, ROUND_BY_ARGUMENT>(y, at + c, v, scale, round_mode);
     }
   }
   if (SHARED && threadIdx.x == 0 && most) atomicMax(&hdr->maxabs32, most);
@@ -370,51 +379,53 @@ column_sum_kernel(const float *part, float *dst, int n, int C) {
   }
 }
 
-// values = payload * 2^s, or the value of an 8-bit code times 2^s; one exponent for every `per` elements.  16 elements a
-// thread where WIDE.
+__device__ __forceinline__ float exponent_scale(int e) {
+  return e >= -126 && e <= 127 ? niti_pow2(e) : ldexpf(1.0f, e < -149 ? -149 : e > 128 ? 128 : e);
+}
+// (an e4m3 code's exponent and fraction, moved into place, are the value over 2^120; exact, the small ones too)
+template <bool E4M3>
+__device__ __forceinline__ float code_value(unsigned b) {
+  if (!E4M3) return (float)(int)(int8_t)b;
+  const float v = __uint_as_float((b & 127u) << 20) * 1.329227995784916e+36f;
+  return (b & 128u) ? -v : v;
+}
+// values = payload * 2^s, or the value of an 8-bit code times 2^s; one exponent for every `per` elements (0: one in all).
+// WIDE: 16 elements a thread, of at most two exponents (per >= 16), in 32-byte stores (whole sectors: half of one a store took
+// 21 us for 8192 x 4096 payloads to bfloat16, this 16); the elements behind the last 16 go to the block behind the others.
 template <int T, bool E4M3, typename S, bool WIDE>
 __global__ void __launch_bounds__(256)
-dequantize_kernel(const uint8_t *q, const S *s, void *out, long long n, Div d_per, long long per) {
+dequantize_kernel(const uint8_t *q, const S *s, void *out, long long n, Div d_per, long long per, int blocks) {
   niti_enter(q, s);
-  constexpr int VEC = WIDE ? 16 : 1;
-  const long long items = n / VEC;
-  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)gridDim.x * 256) {
-    const long long at = i * VEC;
-    // (WIDE: `per` counts vectors and items are below 2^31)
-    const int e = (int)s[per == 0 ? 0 : WIDE ? (long long)div_by((int)i, d_per) : at / per];
-    const float scale = e >= -126 && e <= 127 ? niti_pow2(e) : ldexpf(1.0f, e < -149 ? -149 : e > 128 ? 128 : e);
-    uint8_t b[VEC];
-    if constexpr (WIDE) {
-      const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(q) + i);
-      *reinterpret_cast<uint4 *>(b) = w;
-    } else {
-      b[0] = q[at];
-    }
-    float v[VEC];
+  typedef typename FloatOf<T>::type FT;
+  if (WIDE && (int)blockIdx.x < blocks) {
+    const long long items = n / 16;
+    for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < items; i += (long long)blocks * 256) {
+      const long long at = i * 16;
+      // (indices below 2^31 are divided by multiplication)
+      const long long row = per == 0 ? 0 : d_per.s >= 0 ? (long long)div_by((int)at, d_per) : at / per;
+      const int split = per == 0 || (row + 1) * per - at > 16 ? 16 : (int)((row + 1) * per - at);
+      const float k0 = exponent_scale((int)s[row]), k1 = split < 16 ? exponent_scale((int)s[row + 1]) : k0;
+      const uint4 w4 = __ldcs(reinterpret_cast<const uint4 *>(q) + i);
+      const unsigned w[4] = {w4.x, w4.y, w4.z, w4.w};
+      float v[16];
 #pragma unroll
-    for (int j = 0; j < VEC; ++j) {
-      if (E4M3) {
-        // (the code's exponent and fraction, moved into place, are the value over 2^120; exact, the small ones too)
-        v[j] = __uint_as_float((unsigned)(b[j] & 127) << 20) * 1.329227995784916e+36f * scale;
-        if (b[j] & 128) v[j] = -v[j];
-      } else {
-        v[j] = (float)(int8_t)b[j] * scale;
-      }
-    }
-    if constexpr (WIDE) {
-      // (whole 32-byte sectors: half of one a store took 21 us for 8192 x 4096 payloads to bfloat16)
-      constexpr int PV = 32 / (int)sizeof(typename FloatOf<T>::type);
+      for (int j = 0; j < 16; ++j) v[j] = code_value<E4M3>((w[j >> 2] >> (8 * (j & 3))) & 255u) * (j < split ? k0 : k1);
+      constexpr int PV = 32 / (int)sizeof(FT);
 #pragma unroll
       for (int k = 0; k < 16 / PV; ++k) {
-        unsigned w[8];
-        pack32<T, PV>(v + PV * k, w);
-        store32(reinterpret_cast<typename FloatOf<T>::type *>(out) + at + PV * k, w);
+        unsigned o[8];
+        pack32<T, PV>(v + PV * k, o);
+        store32(reinterpret_cast<FT *>(out) + at + PV * k, o);
       }
-    } else {
-      Pack<T, 1> p;
-      p.set(v);
-      p.store(out, at);
     }
+    return;
+  }
+  const long long from = WIDE ? n / 16 * 16 : 0, step = WIDE ? 256 : (long long)gridDim.x * 256;
+  for (long long at = from + (WIDE ? 0 : (long long)blockIdx.x * 256) + threadIdx.x; at < n; at += step) {
+    const float v[1] = {code_value<E4M3>(q[at]) * exponent_scale((int)s[per == 0 ? 0 : at / per])};
+    Pack<T, 1> p;
+    p.set(v);
+    p.store(out, at);
   }
 }
 
@@ -482,11 +493,16 @@ int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
     constexpr int V16 = 16 / (int)sizeof(typename FloatOf<T>::type);
     auto go = [&](auto shared) -> int {
       constexpr bool SHARED = decltype(shared)::value;
-      auto rows = [&](auto vec, auto nv) -> int {
+      auto rows_as = [&](auto vec, auto nv, auto mode) -> int {
         NITI_CUDA_TRY(ctx, niti_launch(st, row_blocks(ctx, pl.sh, threads, 1024), threads, 0,
-                                       norm_rows_kernel<T, decltype(vec)::value, decltype(nv)::value, NORM, SHARED>, c.x, c.res, c.gain, c.h,
-                                       c.y, c.s_y, rstd, hdr, next, ctx->d_status, pl.sh, c.eps, c.round_mode));
+                                       norm_rows_kernel<T, decltype(vec)::value, decltype(nv)::value, NORM, SHARED, decltype(mode)::value>, c.x, c.res,
+                                       c.gain, c.h, c.y, c.s_y, rstd, hdr, next, ctx->d_status, pl.sh, c.eps, c.round_mode));
         return NITI_OK;
+      };
+      auto rows = [&](auto vec, auto nv) -> int {
+        if constexpr (SHARED || decltype(vec)::value == 1) return rows_as(vec, nv, std::integral_constant<int, ROUND_BY_ARGUMENT>{});
+        else if (c.round_mode == NITI_ROUND_PSR) return rows_as(vec, nv, std::integral_constant<int, NITI_ROUND_PSR>{});
+        else return rows_as(vec, nv, std::integral_constant<int, NITI_ROUND_NEAREST>{});
       };
       auto pick = [&](auto vec) -> int {
         if (pl.nv == 1) return rows(vec, std::integral_constant<int, 1>{});
@@ -506,13 +522,18 @@ int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
     if (r != NITI_OK || c.rows) return r;
     niti_header_passed_on(ctx, next);
     const void *src = NORM && c.res ? c.h : c.x;
-    auto second = [&](auto vec) -> int {
+    auto second_as = [&](auto vec, auto mode) -> int {
       constexpr int VEC = decltype(vec)::value;
       const int parts = (c.C + ROW_THREADS * VEC - 1) / (ROW_THREADS * VEC);
       const long long items = (long long)c.M * parts, cap = 8LL * ctx->sm_count;
-      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(items < cap ? items : cap), ROW_THREADS, 0, norm_round_kernel<T, VEC, NORM>, src,
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(items < cap ? items : cap), ROW_THREADS, 0, norm_round_kernel<T, VEC, NORM, decltype(mode)::value>, src,
                                      c.gain, (const float *)rstd, c.y, c.s_y, (const WsHeader *)hdr, c.M, c.C, parts, c.round_mode));
       return NITI_OK;
+    };
+    auto second = [&](auto vec) -> int {
+      if constexpr (decltype(vec)::value == 1) return second_as(vec, std::integral_constant<int, ROUND_BY_ARGUMENT>{});
+      else if (c.round_mode == NITI_ROUND_PSR) return second_as(vec, std::integral_constant<int, NITI_ROUND_PSR>{});
+      else return second_as(vec, std::integral_constant<int, NITI_ROUND_NEAREST>{});
     };
     r = aligned && c.C % V16 == 0 ? second(std::integral_constant<int, V16>{}) : second(std::integral_constant<int, 1>{});
     ctx->launches++;
@@ -641,17 +662,17 @@ extern "C" int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const
   if (!q || !s || !out || !niti_type_ok(type) || n < 0 || per < 0 || (format != NITI_I8 && format != NITI_E4M3) ||
       (exponent_bytes != 1 && exponent_bytes != 4) || misaligned(out, (uintptr_t)niti_type_size(type)) || misaligned(s, (uintptr_t)exponent_bytes))
     return niti_fail(ctx, NITI_ERR_ARG, "niti_dequantize: bad argument (pointers are aligned to their type)");
-  const bool wide = n % 16 == 0 && per % 16 == 0 && !misaligned(q, 16) && !misaligned(out, 32) && n / 16 < (1LL << 31);
-  const long long items = wide ? n / 16 : n;
-  const long long blocks = (items + 255) / 256, cap = 16LL * ctx->sm_count;
-  const Div d = wide && per ? make_div(per / 16 < (1LL << 31) ? per / 16 : (1LL << 31)) : Div{0u, 0};
+  const bool wide = n >= 16 && (per == 0 || per >= 16) && !misaligned(q, 16) && !misaligned(out, 32);
+  const long long want = ((wide ? n / 16 : n) + 255) / 256, cap = 16LL * ctx->sm_count;
+  const int blocks = (int)(want < cap ? want : cap);
+  const unsigned grid = (unsigned)(blocks + (wide && n % 16 ? 1 : 0));
+  const Div d = per > 0 && n < (1LL << 31) ? make_div(per < (1LL << 31) ? per : (1LL << 31)) : Div{0u, -1};
   const int rc = with_type(type, [&](auto t) -> int {
     constexpr int T = decltype(t)::value;
     auto go = [&](auto e4m3, auto sv, auto w) -> int {
       typedef decltype(sv) S;
-      NITI_CUDA_TRY(ctx, niti_launch((cudaStream_t)stream, (unsigned)(blocks < cap ? blocks : cap), 256, 0,
-                                     dequantize_kernel<T, decltype(e4m3)::value, S, decltype(w)::value>, (const uint8_t *)q, (const S *)s, out,
-                                     (long long)n, d, (long long)per));
+      NITI_CUDA_TRY(ctx, niti_launch((cudaStream_t)stream, grid, 256, 0, dequantize_kernel<T, decltype(e4m3)::value, S, decltype(w)::value>,
+                                     (const uint8_t *)q, (const S *)s, out, (long long)n, d, (long long)per, blocks));
       return NITI_OK;
     };
     auto by_exponent = [&](auto e4m3, auto w) -> int { return exponent_bytes == 1 ? go(e4m3, (int8_t)0, w) : go(e4m3, (int32_t)0, w); };
