@@ -7,11 +7,22 @@ __device__ __forceinline__ float linear_scale(int s) {
   return s >= -126 && s <= 127 ? niti_pow2(s) : s > 127 ? niti_pow2(127) : ldexpf(1.0f, s < -149 ? -149 : s);
 }
 
+// (one instruction each, within two steps of 2^-23; 2^x of -inf is 0, 1 / inf is 0)
+__device__ __forceinline__ float fast_exp2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float fast_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 // The normal distribution's tail for a = |z|: 1 - Phi(a) = t (a1 + t (a2 + ...)) exp(-a^2 / 2) / 2 with t = 1 / (1 + p a / sqrt 2),
 // Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, of Phi half of that).  g receives exp(-a^2 / 2).
-__device__ __forceinline__ float normal_tail(float a, float &g) {
-  const float t = __fdividef(1.0f, fmaf(0.3275911f * 0.70710678f, a, 1.0f));
-  g = __expf(-0.5f * a * a);
+__device__ __forceinline__ float normal_tail(float z, float &g) {
+  const float t = fast_reciprocal(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+  g = fast_exp2(z * -0.72134752f * z);
   float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
   q = fmaf(t, q, 0.5f * 1.421413741f);
   q = fmaf(t, q, 0.5f * -0.284496736f);
@@ -20,17 +31,18 @@ __device__ __forceinline__ float normal_tail(float a, float &g) {
 }
 __device__ __forceinline__ float gelu(float z) {
   float g;
-  const float tail = normal_tail(fabsf(z), g);
+  const float tail = normal_tail(z, g);
   return z * (z < 0.0f ? tail : 1.0f - tail);
 }
 __device__ __forceinline__ float gelu_slope(float z) {
   float g;
-  const float tail = normal_tail(fabsf(z), g);
+  const float tail = normal_tail(z, g);
   return fmaf(z * 0.3989422804f, g, z < 0.0f ? tail : 1.0f - tail);
 }
-__device__ __forceinline__ float silu(float z) { return __fdividef(z, 1.0f + __expf(-z)); }
+__device__ __forceinline__ float sigmoid(float z) { return fast_reciprocal(1.0f + fast_exp2(z * -1.44269504f)); }
+__device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
 __device__ __forceinline__ float silu_slope(float z) {
-  const float s = __fdividef(1.0f, 1.0f + __expf(-z));
+  const float s = sigmoid(z);
   return s * fmaf(z, 1.0f - s, 1.0f);
 }
 __device__ __forceinline__ float act_one(float z, int act) {

@@ -60,7 +60,7 @@ struct niti_ctx {
   // needed would lower the limit under another context of the process)
   size_t smem_optin;
   bool adamw_ready[4];      // shared-memory limits of the optimizer's instances are set
-  bool linear_ready[18];    // attributes of the instances of the float-epilogue kernel are set
+  bool linear_ready[36];    // attributes of the instances of the float-epilogue kernel are set
   int linear_pairs;         // CTA pairs of it that run at once (0: not asked yet)
   int small_ready;          // attributes of the small-multiply kernel are set
   unsigned patience;        // cycles that the blocks of a launch wait for each other (NITI_PATIENCE; 0: test switch)

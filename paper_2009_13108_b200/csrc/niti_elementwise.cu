@@ -1,6 +1,6 @@
 // HBM-bound kernels of the NITI library: the shift-and-round pass (Algorithm 2/3), the integer
 // cross-entropy gradient (Section 3.5), the weight update (Algorithm 1) and the int8 support ops.
-#include "niti_common.cuh"
+#include "niti_pad.cuh"
 #include <mutex>
 
 // ---------------------------------------------------------------------------------------------
@@ -216,38 +216,32 @@ int niti_memset0(niti_ctx *ctx, cudaStream_t st, void *p, size_t bytes) {
 // from the aligned source words around them (bound: latency; for 4096 rows of 1000 bytes one byte per thread took 12.9 us,
 // one output word 6.6 us, this 3.3 us less in the call it belongs to).  src and dst are 16-byte aligned.
 __global__ void __launch_bounds__(256)
-pad_pitch_kernel(const int8_t *__restrict__ src, int8_t *__restrict__ dst, long long rows, int n, int pitch) {
-  niti_enter(src);
-  const unsigned parts = (unsigned)pitch >> 4;
-  for (long long base = (long long)blockIdx.x * blockDim.x; base < rows * parts; base += (long long)gridDim.x * blockDim.x) {
-    // (the division is by thread and 32 bits wide: the block's first row is found once)
-    const long long r0 = base / parts;
-    const unsigned t = (unsigned)(base - r0 * parts) + threadIdx.x, dr = t / parts, part = t - dr * parts;
-    const long long r = r0 + dr;
-    if (r >= rows) continue;
-    const int left = n - 16 * (int)part;                  // valid bytes of this part
-    const long long o = r * n + 16 * part;
-    const int mis = (int)(o & 3);
-    const unsigned *p = reinterpret_cast<const unsigned *>(src) + (o >> 2);
-    unsigned v[5], out[4];
-#pragma unroll
-    for (int k = 0; k < 5; ++k) v[k] = left > 0 && 4 * k < mis + (left < 16 ? left : 16) ? p[k] : 0u;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int have = left - 4 * k;
-      const unsigned w = __funnelshift_r(v[k], v[k + 1], 8u * (unsigned)mis);
-      out[k] = have >= 4 ? w : (have <= 0 ? 0u : w & (0xffffffffu >> (32 - 8 * have)));
-    }
-    *reinterpret_cast<uint4 *>(dst + r * pitch + 16 * part) = make_uint4(out[0], out[1], out[2], out[3]);
-  }
+pad_pitch_kernel(PadJob job) {
+  niti_enter(job.src);
+  niti_pad_rows(job, blockIdx.x, gridDim.x);
+}
+// Two operands in one launch.
+__global__ void __launch_bounds__(256)
+pad_pitch2_kernel(PadJob a, PadJob b, unsigned blocks_a) {
+  niti_enter(a.src, b.src);
+  if (blockIdx.x < blocks_a) niti_pad_rows(a, blockIdx.x, blocks_a);
+  else niti_pad_rows(b, blockIdx.x - blocks_a, gridDim.x - blocks_a);
 }
 
 int niti_launch_pad_pitch(niti_ctx *ctx, cudaStream_t st, const int8_t *src, int8_t *dst, long long rows, int n, int pitch) {
   long long blocks = (rows * (pitch >> 4) + 255) / 256;
   if (blocks > (long long)ctx->sm_count * 16) blocks = (long long)ctx->sm_count * 16;
-  niti_launch(st, (unsigned)blocks, 256, 0, pad_pitch_kernel, src, dst, rows, n, pitch);
+  niti_launch(st, (unsigned)blocks, 256, 0, pad_pitch_kernel, PadJob{src, dst, rows, n, pitch});
   ctx->launches++;
   NITI_CUDA_TRY(ctx, cudaGetLastError());
+  return NITI_OK;
+}
+
+int niti_launch_pad_pitch2(niti_ctx *ctx, cudaStream_t st, const PadJob &a, const PadJob &b) {
+  const long long most = (long long)ctx->sm_count * 8;
+  const unsigned na = niti_pad_blocks(a, 256, most), nb = niti_pad_blocks(b, 256, most);
+  NITI_CUDA_TRY(ctx, niti_launch(st, na + nb, 256, 0, pad_pitch2_kernel, a, b, na));
+  ctx->launches++;
   return NITI_OK;
 }
 

@@ -4,6 +4,8 @@
 #include "niti_act.cuh"
 #include "niti_div.h"
 #include "niti_linear_act.h"
+#include "niti_pad.cuh"
+#include "niti_sums.cuh"
 #include "niti_tcgen05.cuh"
 #include <type_traits>
 
@@ -16,21 +18,34 @@ constexpr int THREADS = 32 * (EPI_WARP0 + EPI_WARPS);
 constexpr int MAX_STAGES = 8, MAX_TBUF = 4;
 constexpr int STG_FLOATS = 32 * 33;                // a warp's buffer for rows that are not whole, aligned vectors
 
+// A multiply of a launch.
 struct Params {
+  int kind;                                        // GK_FC_FWD, GK_FC_DGRAD or GK_FC_WGRAD
   int gm, gn;
-  int bn, nbuf, tmem_cols;
+  int bn;
   int kdepth, ksteps, kb_total, kb_per_split, splits;
-  int stages, nprod;
   int a_bytes, b_bytes, a_boxes, b_boxes, a_box_bytes, b_box_bytes, a_box_step, b_box_step;
   unsigned idesc;
   unsigned long long a_desc, b_desc;
   unsigned a_kstep16, b_kstep16;
   int n_tiles_n, m_units, raster_g, last_group, items;
   Div d_split, d_group, d_units, d_last;
-  int stg_off;                                     // byte offset of the warps' buffers, behind the stages
   int direct;                                      // rows are whole, aligned pieces of 32 bytes
+  int *slabs;                                      // sums of split contractions, and what counts the arrivals of each tile
+  unsigned *counters;
   LinearEpilogue e;
 };
+// A launch: one multiply (forward), or the two of a backward pass, whose items follow one another.
+template <int N>
+struct Launch {
+  Params p[N];
+  int items;
+  int nbuf, bn_most, tmem_cols;                    // accumulators of bn_most columns
+  int stages, nprod, stage_bytes;
+  int stg_off;                                     // byte offset of the warps' buffers, behind the stages
+};
+template <int N>
+struct Maps { CUtensorMap a[N], b[N]; };
 
 __device__ __forceinline__ void decode(const Params &p, int item, int &mu, int &nt, int &split, int &tile) {
   tile = item;
@@ -130,14 +145,31 @@ __device__ __forceinline__ bool epilogue_all(bool ok) {
   return all != 0;
 }
 
+// The copies of a k-block: A and B of this CTA from row m0 / column n0 and contraction element k.
+template <int KIND, int CTAS>
+__device__ __forceinline__ void copy_kblock(const Params &p, const CUtensorMap *ma, const CUtensorMap *mb, unsigned sa, unsigned full, int m0, int n0, int k) {
+  const unsigned sb = sa + p.a_bytes;
+  if (KIND == GK_FC_WGRAD) {
+    for (int j = 0; j < p.a_boxes; ++j) load2<CTAS>(sa + j * p.a_box_bytes, ma, full, m0 + j * p.a_box_step, k);
+  } else {
+    load2<CTAS>(sa, ma, full, k, m0);
+  }
+  if (KIND == GK_FC_FWD) {
+    load2<CTAS>(sb, mb, full, k, n0);
+  } else {
+    for (int j = 0; j < p.b_boxes; ++j) load2<CTAS>(sb + j * p.b_box_bytes, mb, full, n0 + j * p.b_box_step, k);
+  }
+}
+
 // One persistent CTA (or pair on a 256-row tile) per SM; warps 0 - 2 copy, warp 3 multiplies, the others finish tiles.  The
 // pipeline is the one of the integer layers' kernel; nothing here depends on the whole tensor, so that a tile is final when
 // its sums are.  A contraction that is split over CTAs leaves its sums in slabs; the CTA that comes last adds them up, in the
 // order of the splits (integers: any order gives the same), and finishes the tile.
-template <int KIND, int CTAS, int T>
+// N = 2: the error's and the weights' multiply of a backward pass in one launch, whose tiles share the SMs (one after the
+// other they left a seventh of them idle, twice, and each its first copies and its last epilogue uncovered).
+template <int N, int CTAS, int T0, int T1>
 __global__ void __launch_bounds__(THREADS, 1)
-linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Params p, int *slabs,
-              unsigned *counters, WsHeader *next, uint32_t *status) {
+linear_kernel(const __grid_constant__ Maps<N> maps, const __grid_constant__ Launch<N> g, WsHeader *next, uint32_t *status) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ __align__(8) unsigned long long bars[2 * MAX_STAGES + 2 * MAX_TBUF];
   __shared__ unsigned tmem_slot;
@@ -146,16 +178,15 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = (int)threadIdx.x & 31;
   const unsigned rank = CTAS == 2 ? cluster_ctarank() : 0u;
   const unsigned smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const int stage_bytes = p.a_bytes + p.b_bytes;
   const unsigned full0 = smem_u32(&bars[0]), empty0 = smem_u32(&bars[MAX_STAGES]);
   const unsigned tfull0 = smem_u32(&bars[2 * MAX_STAGES]), tempty0 = smem_u32(&bars[2 * MAX_STAGES + MAX_TBUF]);
   const unsigned lead_full0 = CTAS == 2 ? map_to_cta(full0, 0) : full0;
   const unsigned lead_tempty0 = CTAS == 2 ? map_to_cta(tempty0, 0) : tempty0;
   const int first_item = (int)blockIdx.x / CTAS, item_step = (int)gridDim.x / CTAS;
 
-  if (threadIdx.x == 32) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_a) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&map_b) : "memory");
+  if (warp == 1 && lane < 2 * N && g.p[lane % N].items) {
+    const CUtensorMap *m = lane < N ? &maps.a[lane] : &maps.b[lane - N];
+    asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
   }
   if (threadIdx.x == 0) abort_flag = 0;
   if (threadIdx.x < 2 * MAX_STAGES + 2 * MAX_TBUF) {
@@ -165,10 +196,10 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
   }
   if (warp == MMA_WARP) {
     if (CTAS == 2) {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((unsigned)p.tmem_cols) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((unsigned)g.tmem_cols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     } else {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((unsigned)p.tmem_cols) : "memory");
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"((unsigned)g.tmem_cols) : "memory");
       asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
   }
@@ -177,7 +208,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
   if (CTAS == 2) cluster_sync_all();
   tc_fence_after();
   const unsigned tmem_base = tmem_slot;
-  niti_enter(slabs);
+  niti_enter(next);
   if (next && blockIdx.x == 0 && warp == EPI_WARP0 + EPI_WARPS - 1) niti_zero_header(next, lane);
 
   if (warp < PROD_WARPS) {
@@ -185,34 +216,28 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     int stage = 0, owner = 0;
     unsigned phase = 0;
     bool ok = true;
-    const int bn_cta = p.bn / CTAS;
-    const unsigned tx = (unsigned)(CTAS * (p.a_boxes * p.a_box_bytes + p.b_boxes * p.b_box_bytes));
-    for (int item = first_item; ok && item < p.items; item += item_step) {
+    for (int item = first_item; ok && item < g.items; item += item_step) {
+      const int which = N == 2 && item >= g.p[0].items ? 1 : 0;
+      const Params &p = g.p[which];
       int mu, nt, split, tile;
-      decode(p, item, mu, nt, split, tile);
-      const int m0 = (mu * CTAS + (int)rank) * BM, n0 = nt * p.bn + (int)rank * bn_cta;
+      decode(p, which ? item - g.p[0].items : item, mu, nt, split, tile);
+      const int bn_cta = p.bn / CTAS, m0 = (mu * CTAS + (int)rank) * BM, n0 = nt * p.bn + (int)rank * bn_cta;
       const int kb0 = split * p.kb_per_split, kb1 = min(kb0 + p.kb_per_split, p.kb_total);
+      const unsigned tx = (unsigned)(CTAS * (p.a_boxes * p.a_box_bytes + p.b_boxes * p.b_box_bytes));
       for (int kb = kb0; kb < kb1; ++kb) {
         if (owner == warp) {
           if (!mbar_wait_warp(empty0 + 8 * stage, phase ^ 1, &abort_flag, status)) { ok = false; break; }
-          const unsigned full = lead_full0 + 8 * stage, sa = smem_base + stage * stage_bytes, sb = sa + p.a_bytes;
           if (leader) {
+            const unsigned full = lead_full0 + 8 * stage, sa = smem_base + stage * g.stage_bytes;
             if (rank == 0) mbar_expect_tx(full0 + 8 * stage, tx);
             const int k = kb * p.kdepth;
-            if (KIND == GK_FC_WGRAD) {
-              for (int j = 0; j < p.a_boxes; ++j) load2<CTAS>(sa + j * p.a_box_bytes, &map_a, full, m0 + j * p.a_box_step, k);
-            } else {
-              load2<CTAS>(sa, &map_a, full, k, m0);
-            }
-            if (KIND == GK_FC_FWD) {
-              load2<CTAS>(sb, &map_b, full, k, n0);
-            } else {
-              for (int j = 0; j < p.b_boxes; ++j) load2<CTAS>(sb + j * p.b_box_bytes, &map_b, full, n0 + j * p.b_box_step, k);
-            }
+            if (N == 1) copy_kblock<GK_FC_FWD, CTAS>(p, &maps.a[0], &maps.b[0], sa, full, m0, n0, k);
+            else if (p.kind == GK_FC_DGRAD) copy_kblock<GK_FC_DGRAD, CTAS>(p, &maps.a[which], &maps.b[which], sa, full, m0, n0, k);
+            else copy_kblock<GK_FC_WGRAD, CTAS>(p, &maps.a[which], &maps.b[which], sa, full, m0, n0, k);
           }
         }
-        if (++owner == p.nprod) owner = 0;
-        if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        if (++owner == g.nprod) owner = 0;
+        if (++stage == g.stages) { stage = 0; phase ^= 1; }
       }
     }
   } else if (warp == MMA_WARP) {
@@ -221,20 +246,23 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
       int stage = 0;
       unsigned phase = 0, buf = 0, par = 0;
       bool ok = true;
-      const unsigned a_lo0 = (unsigned)p.a_desc, b_lo0 = (unsigned)p.b_desc, a_hi = (unsigned)(p.a_desc >> 32), b_hi = (unsigned)(p.b_desc >> 32);
-      const unsigned ak = p.a_kstep16, bk = p.b_kstep16, idesc = p.idesc, a_bytes = (unsigned)p.a_bytes;
-      const int ksteps = p.ksteps;
-      for (int item = first_item; ok && item < p.items; item += item_step) {
-        const int split = p.splits > 1 ? item - div_by(item, p.d_split) * p.splits : 0;
+      for (int item = first_item; ok && item < g.items; item += item_step) {
+        const int which = N == 2 && item >= g.p[0].items ? 1 : 0;
+        const Params &p = g.p[which];
+        const int in = which ? item - g.p[0].items : item;
+        const unsigned a_lo0 = (unsigned)p.a_desc, b_lo0 = (unsigned)p.b_desc, a_hi = (unsigned)(p.a_desc >> 32), b_hi = (unsigned)(p.b_desc >> 32);
+        const unsigned ak = p.a_kstep16, bk = p.b_kstep16, idesc = p.idesc, a_bytes = (unsigned)p.a_bytes;
+        const int ksteps = p.ksteps;
+        const int split = p.splits > 1 ? in - div_by(in, p.d_split) * p.splits : 0;
         const int kb0 = split * p.kb_per_split, kb1 = min(kb0 + p.kb_per_split, p.kb_total);
         if (!mbar_wait_warp(tempty0 + 8 * buf, par ^ 1u, &abort_flag, status)) { ok = false; break; }
-        const unsigned tfull = tfull0 + 8 * buf, tmem_d = tmem_base + buf * (unsigned)p.bn;
-        if (++buf == (unsigned)p.nbuf) { buf = 0; par ^= 1u; }
+        const unsigned tfull = tfull0 + 8 * buf, tmem_d = tmem_base + buf * (unsigned)g.bn_most;
+        if (++buf == (unsigned)g.nbuf) { buf = 0; par ^= 1u; }
         tc_fence_after();
         for (int kb = kb0; kb < kb1; ++kb) {
           if (!mbar_wait_warp(full0 + 8 * stage, phase, &abort_flag, status)) { ok = false; break; }
           tc_fence_after();
-          const unsigned sa = smem_base + stage * stage_bytes;
+          const unsigned sa = smem_base + stage * g.stage_bytes;
           const unsigned a_lo = a_lo0 + ((sa >> 4) & 0x3fff), b_lo = b_lo0 + (((sa + a_bytes) >> 4) & 0x3fff);
           const unsigned acc = kb > kb0 ? 1u : 0u;
           if (leader) {
@@ -243,7 +271,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
             else issue_kblock<CTAS, 1>(tmem_d, a_lo, a_hi, b_lo, b_hi, ak, bk, idesc, acc);
             if (CTAS == 2) tc_commit_pair(empty0 + 8 * stage); else tc_commit(empty0 + 8 * stage);
           }
-          if (++stage == p.stages) { stage = 0; phase ^= 1; }
+          if (++stage == g.stages) { stage = 0; phase ^= 1; }
         }
         if (ok && leader) {
           if (CTAS == 2) tc_commit_pair(tfull); else tc_commit(tfull);
@@ -252,37 +280,42 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
     }
   } else {
     const int ew = warp - EPI_WARP0, quarter = warp & 3, part = ew >> 2;
-    float *stg = reinterpret_cast<float *>(smem_raw + (smem_base - smem_u32(smem_raw)) + p.stg_off) + ew * STG_FLOATS;
-    const LinearEpilogue &e = p.e;
-    const int s_col = (e.s1 ? *e.s1 : 0);
+    float *stg = reinterpret_cast<float *>(smem_raw + (smem_base - smem_u32(smem_raw)) + g.stg_off) + ew * STG_FLOATS;
     unsigned buf = 0, par = 0;
     bool wide_exp = false;
-    for (int item = first_item; item < p.items; item += item_step) {
+    for (int item = first_item; item < g.items; item += item_step) {
+      const int which = N == 2 && item >= g.p[0].items ? 1 : 0;
+      const Params &p = g.p[which];
+      const LinearEpilogue &e = p.e;
       int mu, nt, split, tile;
-      decode(p, item, mu, nt, split, tile);
+      decode(p, which ? item - g.p[0].items : item, mu, nt, split, tile);
       const int row0 = (mu * CTAS + (int)rank) * BM + 32 * quarter, n0 = nt * p.bn;
       const int row = row0 + lane < p.gm ? row0 + lane : p.gm - 1;
-      const int s = e.s0[e.s0_rows ? row : 0] + s_col;
+      const int s = e.s0[e.s0_rows ? row : 0] + *e.s1;
       wide_exp |= s < -128 || s > 127;
       const float f = linear_scale(s);
       bool ok = mbar_wait_warp(tfull0 + 8 * buf, par, &abort_flag, status);
       if (p.splits > 1) ok = epilogue_all(ok);     // (they meet at barriers below: all go on, or none)
       if (!ok) break;
       tc_fence_after();
-      const unsigned tm = tmem_base + buf * (unsigned)p.bn + ((unsigned)(32 * quarter) << 16);
+      const unsigned tm = tmem_base + buf * (unsigned)g.bn_most + ((unsigned)(32 * quarter) << 16);
       const unsigned tempty = lead_tempty0 + 8 * buf;
-      if (++buf == (unsigned)p.nbuf) { buf = 0; par ^= 1u; }
+      if (++buf == (unsigned)g.nbuf) { buf = 0; par ^= 1u; }
       auto drained = [&]() {
         tc_fence_before();
         __syncwarp();
         if (lane == 0) { if (CTAS == 2) mbar_arrive_cluster(tempty); else mbar_arrive(tempty); }
+      };
+      auto finish = [&](int (&v)[32], int c) {
+        if (T0 == T1 || which == 0) finish_chunk<T0>(p, v, row0, n0 + 32 * c, f, stg, lane);
+        else finish_chunk<T1>(p, v, row0, n0 + 32 * c, f, stg, lane);
       };
       if (p.splits == 1) {
         for (int c = part; c < p.bn / 32; c += EPI_WARPS / 4) {
           int v[32];
           if (n0 + 32 * c < p.gn) {
             tc_ld32(tm + 32u * (unsigned)c, v);
-            finish_chunk<T>(p, v, row0, n0 + 32 * c, f, stg, lane);
+            finish(v, c);
           }
         }
         drained();
@@ -290,7 +323,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
       }
       // a share of a split contraction: 32 columns x 128 rows of sums in column order
       const int slot = tile * CTAS + (int)rank, words = p.bn * BM;
-      int *mine = slabs + ((long long)slot * p.splits + split) * words + 32 * quarter + lane;
+      int *mine = p.slabs + ((long long)slot * p.splits + split) * words + 32 * quarter + lane;
       for (int c = part; c < p.bn / 32; c += EPI_WARPS / 4) {
         int v[32];
         tc_ld32(tm + 32u * (unsigned)c, v);
@@ -301,13 +334,13 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
       __threadfence();
       asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
       if (ew == 0 && lane == 0) {
-        const unsigned before = atomicAdd(counters + slot, 1u);
+        const unsigned before = atomicAdd(p.counters + slot, 1u);
         __threadfence();
         is_last = before == (unsigned)p.splits - 1u;
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");
       if (is_last) {
-        const int *all = slabs + (long long)slot * p.splits * words + 32 * quarter + lane;
+        const int *all = p.slabs + (long long)slot * p.splits * words + 32 * quarter + lane;
         for (int c = part; c < p.bn / 32; c += EPI_WARPS / 4) {
           if (n0 + 32 * c >= p.gn) continue;
           int v[32];
@@ -317,7 +350,7 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += __ldcg(all + (long long)k * words + (32 * c + j) * BM);
           }
-          finish_chunk<T>(p, v, row0, n0 + 32 * c, f, stg, lane);
+          finish(v, c);
         }
       }
       asm volatile("bar.sync 1, %0;" ::"n"(32 * EPI_WARPS) : "memory");          // (is_last has been read by all)
@@ -336,14 +369,18 @@ linear_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__
   if (CTAS == 2) cluster_sync_all();
   if (warp == MMA_WARP) {
     tc_fence_after();
-    if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((unsigned)p.tmem_cols) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((unsigned)p.tmem_cols) : "memory");
+    if (CTAS == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((unsigned)g.tmem_cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((unsigned)g.tmem_cols) : "memory");
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------
 // Cycles of a k-block of 128 contraction elements: multiplies, or the operand copies (constants as measured for the integer
 // layers' kernel: 84 bytes a clock into one SM, 9000 into all).
+bool direct_rows(const LinearMultiply &x) {
+  const uintptr_t ptrs = (uintptr_t)x.e.out | (uintptr_t)x.e.res | (uintptr_t)x.e.z;
+  return (x.gn * niti_type_size(x.type)) % 32 == 0 && (ptrs & 31) == 0 && ((uintptr_t)x.e.bias & 15) == 0;
+}
 double kblock_cycles(int ctas, int bn, int ksteps, long long running) {
   const double mma = bn / 2.0, smem = 32.0 + bn / (4.0 * ctas), bytes = (128.0 + (double)bn / ctas) * 32.0 * ksteps;
   double c = ksteps * (mma > smem ? mma : smem);
@@ -352,43 +389,39 @@ double kblock_cycles(int ctas, int bn, int ksteps, long long running) {
   return c < 100.0 * ksteps ? 100.0 * ksteps : c;
 }
 
-struct Choice { int ctas, bn, splits; };
-// Tile width, pairs and splits with the least modelled time: k-blocks of a wave, the epilogue of its tiles (about 20 issue
-// slots an element, hidden behind the next tile's main loop), and for splits the slabs' way through L2.
-Choice choose(const niti_ctx *ctx, int kind, long long gm, long long gn, int kb, int ksteps, int pairs) {
-  Choice best = {1, 32, 1};
-  double least = 1e300;
-  const long long mt = (gm + BM - 1) / BM;
-  const int unit = kind == GK_FC_FWD ? 32 : 64;
-  for (int ctas = 1; ctas <= 2; ++ctas) {
-    if (ctas == 2 && mt < 2) break;
-    const long long mu = (mt + ctas - 1) / ctas, units = ctas == 2 ? pairs : ctx->sm_count;
-    for (int bn = 256; bn >= unit; bn -= unit) {
-      if (bn > 32 && bn - unit >= gn && bn > unit) continue;
-      if (bn / ctas % 16) continue;
-      const long long tiles = mu * ((gn + bn - 1) / bn);
-      const double epi = 20.0 * bn;
-      for (int s = 1; s <= 32; s += s < 4 ? 1 : s < 8 ? 2 : 4) {
-        if (s > 1 && (tiles * s > units || kb / s < 4 || tiles * ctas > NITI_LINEAR_COUNTERS || ctx->sm_count > NITI_LINEAR_MAX_SMS)) break;
-        const long long items = tiles * s, waves = (items + units - 1) / units;
-        const double main = ((kb + s - 1) / s) * kblock_cycles(ctas, bn, ksteps, (items < units ? items : units) * ctas);
-        double t = main + (double)(waves - 1) * (main > epi ? main : epi) + epi + (ctas == 2 ? 1500.0 : 0.0);
-        if (s > 1) t += 3000.0 + 8.0 * bn * (s + 1);
-        if (t < least * 0.98) { least = t; best = {ctas, bn, s}; }
-      }
+struct Choice { int bn, splits; double cycles; };
+// Tile width and splits with the least modelled time on `units` CTAs (pairs): k-blocks of a wave, the epilogue of its tiles
+// (issue slots an element, hidden behind the next tile's main loop), and for splits the slabs' way through L2.
+Choice choose(const niti_ctx *ctx, const LinearMultiply &x, int ctas, long long units, double epi_slots) {
+  Choice best = {32, 1, 1e300};
+  const int kdepth = pick_swizzle(x.gk), ksteps = kdepth / 32, kb = (int)((x.gk + kdepth - 1) / kdepth);
+  const long long mu = ((x.gm + BM - 1) / BM + ctas - 1) / ctas;
+  const int unit = x.kind == GK_FC_FWD ? 32 : 64;
+  for (int bn = 256; bn >= unit; bn -= unit) {
+    if (bn > unit && bn - unit >= x.gn) continue;
+    if (bn / ctas % 16) continue;
+    const long long tiles = mu * ((x.gn + bn - 1) / bn);
+    const double epi = epi_slots * bn;
+    for (int s = 1; s <= 32; s += s < 4 ? 1 : s < 8 ? 2 : 4) {
+      if (s > 1 && (tiles * s > units || kb / s < 4 || tiles * ctas > NITI_LINEAR_COUNTERS || ctx->sm_count > NITI_LINEAR_MAX_SMS)) break;
+      const long long items = tiles * s, waves = (items + units - 1) / units;
+      const double main = ((kb + s - 1) / s) * kblock_cycles(ctas, bn, ksteps, (items < units ? items : units) * ctas);
+      double t = main + (double)(waves - 1) * (main > epi ? main : epi) + epi + (ctas == 2 ? 1500.0 : 0.0);
+      if (s > 1) t += 3000.0 + 8.0 * bn * (s + 1);
+      if (t < best.cycles * 0.98) best = {bn, s, t};
     }
   }
   return best;
 }
 
-template <int KIND, int CTAS, int T>
+template <int N, int CTAS, int T0, int T1>
 int set_up(niti_ctx *ctx) {
   // (per device and instance, the same value in every context: see niti_ctx::smem_optin)
-  bool &ready = ctx->linear_ready[(KIND * 2 + CTAS - 1) * 3 + T];
+  bool &ready = ctx->linear_ready[((N - 1) * 2 + CTAS - 1) * 9 + 3 * T0 + T1];
   if (ready) return NITI_OK;
   cudaFuncAttributes fa;
-  NITI_CUDA_TRY(ctx, cudaFuncGetAttributes(&fa, linear_kernel<KIND, CTAS, T>));
-  NITI_CUDA_TRY(ctx, cudaFuncSetAttribute(linear_kernel<KIND, CTAS, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  NITI_CUDA_TRY(ctx, cudaFuncGetAttributes(&fa, linear_kernel<N, CTAS, T0, T1>));
+  NITI_CUDA_TRY(ctx, cudaFuncSetAttribute(linear_kernel<N, CTAS, T0, T1>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                           (int)(ctx->smem_optin - fa.sharedSizeBytes)));
   ready = true;
   return NITI_OK;
@@ -397,7 +430,7 @@ int set_up(niti_ctx *ctx) {
 // CTA pairs that run at once (SMs pair up inside a GPC, so there can be fewer than half of the SMs).
 int ask_pairs(niti_ctx *ctx) {
   if (ctx->linear_pairs) return NITI_OK;
-  const int rc = set_up<GK_FC_FWD, 2, NITI_BF16>(ctx);
+  const int rc = set_up<1, 2, NITI_BF16, NITI_BF16>(ctx);
   if (rc != NITI_OK) return rc;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
@@ -412,15 +445,14 @@ int ask_pairs(niti_ctx *ctx) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int n = 0;
-  NITI_CUDA_TRY(ctx, cudaOccupancyMaxActiveClusters(&n, linear_kernel<GK_FC_FWD, 2, NITI_BF16>, &cfg));
+  NITI_CUDA_TRY(ctx, cudaOccupancyMaxActiveClusters(&n, linear_kernel<1, 2, NITI_BF16, NITI_BF16>, &cfg));
   ctx->linear_pairs = n < 1 ? 1 : n < ctx->sm_count / 2 ? n : ctx->sm_count / 2;
   return NITI_OK;
 }
 
-template <int KIND, int CTAS, int T>
-int launch_as(niti_ctx *ctx, cudaStream_t st, const Params &p, const CUtensorMap &ma, const CUtensorMap &mb, size_t smem, unsigned grid, int *slabs,
-              unsigned *counters, WsHeader *next) {
-  const int rc = set_up<KIND, CTAS, T>(ctx);
+template <int N, int CTAS, int T0, int T1>
+int launch_as(niti_ctx *ctx, cudaStream_t st, const Launch<N> &g, const Maps<N> &maps, size_t smem, unsigned grid, WsHeader *next) {
+  const int rc = set_up<N, CTAS, T0, T1>(ctx);
   if (rc != NITI_OK) return rc;
   cudaLaunchConfig_t cfg;
   memset(&cfg, 0, sizeof(cfg));
@@ -437,50 +469,42 @@ int launch_as(niti_ctx *ctx, cudaStream_t st, const Params &p, const CUtensorMap
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  NITI_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, linear_kernel<KIND, CTAS, T>, ma, mb, p, slabs, counters, next, ctx->d_status));
+  NITI_CUDA_TRY(ctx, cudaLaunchKernelEx(&cfg, linear_kernel<N, CTAS, T0, T1>, maps, g, next, ctx->d_status));
   ctx->launches++;
   ctx->tc_launches++;
   if (CTAS == 2) ctx->tc2_launches++;
   return NITI_OK;
 }
 
-}  // namespace
-
-int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0, long long ld0, const int8_t *p1, long long ld1, long long gm,
-                     long long gn, long long gk, const LinearEpilogue &e, int type, int *slabs, unsigned *counters, WsHeader *next) {
-  Params p;
-  memset(&p, 0, sizeof(p));
-  p.gm = (int)gm; p.gn = (int)gn;
-  p.e = e;
-  p.kdepth = pick_swizzle(gk);
-  p.ksteps = p.kdepth / 32;
-  p.kb_total = (int)((gk + p.kdepth - 1) / p.kdepth);
-  const int rc = ask_pairs(ctx);
-  if (rc != NITI_OK) return rc;
-  const int pairs = ctx->linear_pairs;
-  const Choice c = choose(ctx, kind, gm, gn, p.kb_total, p.ksteps, pairs);
-  const int ctas = c.ctas;
+// Parameters and tensor maps of one multiply; false: an operand has no tensor map.
+bool fill(niti_ctx *ctx, const LinearMultiply &x, int ctas, const Choice &c, Params &p, CUtensorMap &ma, CUtensorMap &mb) {
+  p.kind = x.kind;
+  p.gm = (int)x.gm; p.gn = (int)x.gn;
+  p.e = x.e;
   p.bn = c.bn;
+  p.kdepth = pick_swizzle(x.gk);
+  p.ksteps = p.kdepth / 32;
+  p.kb_total = (int)((x.gk + p.kdepth - 1) / p.kdepth);
   p.kb_per_split = (p.kb_total + c.splits - 1) / c.splits;
   p.splits = (p.kb_total + p.kb_per_split - 1) / p.kb_per_split;
   const int bn_cta = p.bn / ctas;
   MapSpec sa, sb;
   memset(&sa, 0, sizeof(sa));
   memset(&sb, 0, sizeof(sb));
-  const bool a_mn = kind == GK_FC_WGRAD, b_mn = kind != GK_FC_FWD;
+  const bool a_mn = x.kind == GK_FC_WGRAD, b_mn = x.kind != GK_FC_FWD;
   int a_sw = p.kdepth, b_sw = p.kdepth;
   if (a_mn) {
-    a_sw = pick_swizzle(gm);
-    sa = {2, {(cuuint64_t)gm, (cuuint64_t)gk}, {(cuuint64_t)ld0}, {(cuuint32_t)a_sw, (cuuint32_t)p.kdepth}, a_sw, p0};
+    a_sw = pick_swizzle(x.gm);
+    sa = {2, {(cuuint64_t)x.gm, (cuuint64_t)x.gk}, {(cuuint64_t)x.ld0}, {(cuuint32_t)a_sw, (cuuint32_t)p.kdepth}, a_sw, x.p0};
     p.a_boxes = BM / a_sw;
-    if ((long long)p.a_boxes * a_sw > (gm + a_sw - 1) / a_sw * a_sw) p.a_boxes = (int)((gm + a_sw - 1) / a_sw);
+    if ((long long)p.a_boxes * a_sw > (x.gm + a_sw - 1) / a_sw * a_sw) p.a_boxes = (int)((x.gm + a_sw - 1) / a_sw);
     p.a_box_bytes = p.kdepth * a_sw;
     p.a_box_step = a_sw;
     p.a_bytes = (BM / a_sw) * p.a_box_bytes;
     p.a_desc = desc_mnmajor(a_sw, p.kdepth);
     p.a_kstep16 = (unsigned)((32 * a_sw) >> 4);
   } else {
-    sa = {2, {(cuuint64_t)gk, (cuuint64_t)gm}, {(cuuint64_t)ld0}, {(cuuint32_t)p.kdepth, BM}, a_sw, p0};
+    sa = {2, {(cuuint64_t)x.gk, (cuuint64_t)x.gm}, {(cuuint64_t)x.ld0}, {(cuuint32_t)p.kdepth, BM}, a_sw, x.p0};
     p.a_boxes = 1;
     p.a_box_bytes = p.a_bytes = BM * p.kdepth;
     p.a_desc = desc_kmajor(a_sw);
@@ -488,7 +512,7 @@ int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0,
   }
   if (b_mn) {
     b_sw = pick_swizzle_mn(bn_cta);
-    sb = {2, {(cuuint64_t)gn, (cuuint64_t)gk}, {(cuuint64_t)ld1}, {(cuuint32_t)b_sw, (cuuint32_t)p.kdepth}, b_sw, p1};
+    sb = {2, {(cuuint64_t)x.gn, (cuuint64_t)x.gk}, {(cuuint64_t)x.ld1}, {(cuuint32_t)b_sw, (cuuint32_t)p.kdepth}, b_sw, x.p1};
     p.b_boxes = (bn_cta + b_sw - 1) / b_sw;
     p.b_box_bytes = p.kdepth * b_sw;
     p.b_box_step = b_sw;
@@ -496,7 +520,7 @@ int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0,
     p.b_desc = desc_mnmajor(b_sw, p.kdepth);
     p.b_kstep16 = (unsigned)((32 * b_sw) >> 4);
   } else {
-    sb = {2, {(cuuint64_t)gk, (cuuint64_t)gn}, {(cuuint64_t)ld1}, {(cuuint32_t)p.kdepth, (cuuint32_t)bn_cta}, b_sw, p1};
+    sb = {2, {(cuuint64_t)x.gk, (cuuint64_t)x.gn}, {(cuuint64_t)x.ld1}, {(cuuint32_t)p.kdepth, (cuuint32_t)bn_cta}, b_sw, x.p1};
     p.b_boxes = 1;
     p.b_box_bytes = p.b_bytes = bn_cta * p.kdepth;
     p.b_desc = desc_kmajor(b_sw);
@@ -504,57 +528,98 @@ int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0,
   }
   p.a_bytes = (p.a_bytes + 1023) / 1024 * 1024;
   p.b_bytes = (p.b_bytes + 1023) / 1024 * 1024;
-  const int es = niti_type_size(type);
-  const uintptr_t ptrs = (uintptr_t)e.out | (uintptr_t)e.res | (uintptr_t)e.z;
-  p.direct = (gn * es) % 32 == 0 && (ptrs & 31) == 0 && ((uintptr_t)e.bias & 15) == 0;
-  const int stg = p.direct ? 0 : EPI_WARPS * STG_FLOATS * 4;
-  const int stage = p.a_bytes + p.b_bytes;
-  p.stages = (216 * 1024 - stg) / stage;
-  if (p.stages > MAX_STAGES) p.stages = MAX_STAGES;
-  if (p.stages == 5 || p.stages == 7) p.stages -= 1;
-  if (p.stages < 2) return niti_fail(ctx, NITI_ERR_SHAPE, "linear layer: no room for two stages");
-  p.stg_off = p.stages * stage;
-  p.nprod = 1;
-  for (int d = 2; d <= PROD_WARPS; ++d)
-    if (p.stages % d == 0) p.nprod = d;
-  p.nbuf = 512 / p.bn > MAX_TBUF ? MAX_TBUF : 512 / p.bn;
-  p.tmem_cols = 32;
-  while (p.tmem_cols < p.nbuf * p.bn) p.tmem_cols <<= 1;
+  p.direct = direct_rows(x) ? 1 : 0;
   // instruction descriptor: s32 accumulate, signed 8-bit operands, majorness, N, M
   p.idesc = (2u << 4) | (1u << 7) | (1u << 10) | ((unsigned)a_mn << 15) | ((unsigned)b_mn << 16) | ((unsigned)(p.bn >> 3) << 17) |
             ((unsigned)((BM * ctas) >> 4) << 24);
-  const long long mt = (gm + BM - 1) / BM;
+  const long long mt = (x.gm + BM - 1) / BM;
   p.m_units = (int)((mt + ctas - 1) / ctas);
-  p.n_tiles_n = (int)((gn + p.bn - 1) / p.bn);
-  const long long items = (long long)p.m_units * p.n_tiles_n * p.splits;
-  if (items >= (1LL << 30)) return niti_fail(ctx, NITI_ERR_SHAPE, "linear layer: too many tiles");
-  p.items = (int)items;
+  p.n_tiles_n = (int)((x.gn + p.bn - 1) / p.bn);
+  p.items = (int)((long long)p.m_units * p.n_tiles_n * p.splits);
   p.raster_g = ctas == 2 ? 8 : 12;
   p.last_group = (p.m_units - 1) / p.raster_g;
   p.d_split = make_div(p.splits);
   p.d_group = make_div((long long)p.raster_g * p.n_tiles_n);
   p.d_units = make_div(p.raster_g);
   p.d_last = make_div(p.m_units - p.last_group * p.raster_g);
-  CUtensorMap ma, mb;
-  if (!encode(ctx, &ma, sa) || !encode(ctx, &mb, sb)) return niti_fail(ctx, NITI_ERR_CUDA, "linear layer: no tensor map for an operand");
-  const size_t smem = (size_t)p.stg_off + stg + 1024;
-  const long long units = ctas == 2 ? pairs : ctx->sm_count;
-  const unsigned grid = (unsigned)((items < units ? items : units) * ctas);
-  auto with_kind = [&](auto kc) -> int {
-    constexpr int KIND = decltype(kc)::value;
-    auto with = [&](auto tc) -> int {
-      constexpr int T = decltype(tc)::value;
-      return ctas == 2 ? launch_as<KIND, 2, T>(ctx, st, p, ma, mb, smem, grid, slabs, counters, next)
-                       : launch_as<KIND, 1, T>(ctx, st, p, ma, mb, smem, grid, slabs, counters, next);
-    };
-    if (type == NITI_F32) return with(std::integral_constant<int, NITI_F32>{});
-    if (type == NITI_BF16) return with(std::integral_constant<int, NITI_BF16>{});
-    return with(std::integral_constant<int, NITI_F16>{});
-  };
-  if (kind == GK_FC_FWD) return with_kind(std::integral_constant<int, GK_FC_FWD>{});
-  if (kind == GK_FC_DGRAD) return with_kind(std::integral_constant<int, GK_FC_DGRAD>{});
-  return with_kind(std::integral_constant<int, GK_FC_WGRAD>{});
+  return encode(ctx, &ma, sa) && encode(ctx, &mb, sb);
 }
+
+template <int N>
+int run_multiplies(niti_ctx *ctx, cudaStream_t st, const LinearMultiply *x, int *slabs, unsigned *counters, WsHeader *next) {
+  int rc = ask_pairs(ctx);
+  if (rc != NITI_OK) return rc;
+  // each of two multiplies is planned for its share of the SMs (they have the same number of operations)
+  Choice c[2][N];
+  double cycles[2] = {0.0, 0.0};
+  int wanted = 0;
+  for (int i = 0; i < N; ++i) wanted += x[i].e.out ? 1 : 0;
+  for (int ctas = 1; ctas <= 2; ++ctas)
+    for (int i = 0; i < N; ++i) {
+      if (!x[i].e.out) continue;
+      const long long units = (ctas == 2 ? ctx->linear_pairs : ctx->sm_count) / wanted;
+      c[ctas - 1][i] = choose(ctx, x[i], ctas, units < 1 ? 1 : units, direct_rows(x[i]) ? 20.0 : 40.0);
+      if (c[ctas - 1][i].cycles > cycles[ctas - 1]) cycles[ctas - 1] = c[ctas - 1][i].cycles;
+      if (ctas == 2 && x[i].gm <= BM) cycles[1] = 1e300;
+    }
+  const int ctas = cycles[1] < cycles[0] ? 2 : 1;
+  Launch<N> g;
+  Maps<N> maps;
+  memset(&g, 0, sizeof(g));
+  bool staged = false;
+  long long items = 0;
+  for (int i = 0; i < N; ++i) {
+    Params &p = g.p[i];
+    if (((x[i].gm + BM - 1) / BM) * ((x[i].gn + 31) / 32) >= (1LL << 28)) return niti_fail(ctx, NITI_ERR_SHAPE, "linear layer: too many tiles");
+    if (!x[i].e.out) {                             // (not wanted)
+      memset(&maps.a[i], 0, sizeof(maps.a[i]));
+      memset(&maps.b[i], 0, sizeof(maps.b[i]));
+      continue;
+    }
+    if (!fill(ctx, x[i], ctas, c[ctas - 1][i], p, maps.a[i], maps.b[i])) return niti_fail(ctx, NITI_ERR_CUDA, "linear layer: no tensor map for an operand");
+    p.slabs = slabs;
+    p.counters = counters;
+    if (p.splits > 1) {                            // (at most a tile of 128 x 256 words for every SM that the multiply was planned for)
+      slabs += (size_t)p.items * ctas * BM * p.bn;
+      counters += NITI_LINEAR_COUNTERS;
+    }
+    items += p.items;
+    if (p.a_bytes + p.b_bytes > g.stage_bytes) g.stage_bytes = p.a_bytes + p.b_bytes;
+    if (p.bn > g.bn_most) g.bn_most = p.bn;
+    staged = staged || !p.direct;
+  }
+  g.items = (int)items;
+  const int stg = staged ? EPI_WARPS * STG_FLOATS * 4 : 0;
+  g.stages = (216 * 1024 - stg) / g.stage_bytes;
+  if (g.stages > MAX_STAGES) g.stages = MAX_STAGES;
+  if (g.stages == 5 || g.stages == 7) g.stages -= 1;
+  if (g.stages < 2) return niti_fail(ctx, NITI_ERR_SHAPE, "linear layer: no room for two stages");
+  g.stg_off = g.stages * g.stage_bytes;
+  g.nprod = 1;
+  for (int d = 2; d <= PROD_WARPS; ++d)
+    if (g.stages % d == 0) g.nprod = d;
+  g.nbuf = 512 / g.bn_most > MAX_TBUF ? MAX_TBUF : 512 / g.bn_most;
+  g.tmem_cols = 32;
+  while (g.tmem_cols < g.nbuf * g.bn_most) g.tmem_cols <<= 1;
+  const size_t smem = (size_t)g.stg_off + stg + 1024;
+  const long long units = ctas == 2 ? ctx->linear_pairs : ctx->sm_count;
+  const unsigned grid = (unsigned)((items < units ? items : units) * ctas);
+  auto go = [&](auto t0, auto t1) -> int {
+    constexpr int T0 = decltype(t0)::value, T1 = decltype(t1)::value;
+    return ctas == 2 ? launch_as<N, 2, T0, T1>(ctx, st, g, maps, smem, grid, next) : launch_as<N, 1, T0, T1>(ctx, st, g, maps, smem, grid, next);
+  };
+  auto with = [](int type, auto f) -> int {
+    if (type == NITI_F32) return f(std::integral_constant<int, NITI_F32>{});
+    if (type == NITI_BF16) return f(std::integral_constant<int, NITI_BF16>{});
+    return f(std::integral_constant<int, NITI_F16>{});
+  };
+  return with(x[0].type, [&](auto t0) -> int {
+    if constexpr (N == 1) return go(t0, t0);
+    else return with(x[N - 1].type, [&](auto t1) -> int { return go(t0, t1); });
+  });
+}
+
+}  // namespace
 
 // ---- the error of the backward pass ---------------------------------------------------------
 namespace {
@@ -562,37 +627,59 @@ namespace {
 constexpr int ERR_THREADS = 128;
 constexpr unsigned INF_BITS = 0x7f800000u;
 
-// e = dout act'(z) of a block's rows and columns, a thread on the same VEC columns in every row.
+// e = dout act'(z) of a block's rows and columns, a thread on the same VEC columns in every row; two rows at work and two on
+// their way.
 template <int T, int VEC, int ACT, typename F>
 __device__ __forceinline__ void error_rows(const void *dout, const void *z, int N, int r0, int r1, int c, F take) {
-  constexpr int DEEP = 4;                          // rows in flight
-  for (int r = r0; r < r1; r += DEEP) {
-    Pack<T, VEC> d[DEEP], zz[DEEP];
+  constexpr int DEEP = 2;
+  Pack<T, VEC> d[2][DEEP], zz[2][DEEP];
+  auto fetch = [&](int r, Pack<T, VEC> (&dd)[DEEP], Pack<T, VEC> (&zd)[DEEP]) {
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
-        d[k].load(dout, (long long)(r + k) * N + c);
-        if (ACT != NITI_ACT_NONE) zz[k].load(z, (long long)(r + k) * N + c);
+        dd[k].load(dout, (long long)(r + k) * N + c);
+        if (ACT != NITI_ACT_NONE) zd[k].load(z, (long long)(r + k) * N + c);
       }
+  };
+  auto work = [&](int r, const Pack<T, VEC> (&dd)[DEEP], const Pack<T, VEC> (&zd)[DEEP]) {
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
         float e[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) e[j] = ACT == NITI_ACT_NONE ? d[k].get(j) : d[k].get(j) * act_slope(zz[k].get(j), ACT);
+        for (int j = 0; j < VEC; ++j) e[j] = ACT == NITI_ACT_NONE ? dd[k].get(j) : dd[k].get(j) * act_slope(zd[k].get(j), ACT);
         take(r + k, e);
       }
+  };
+  fetch(r0, d[0], zz[0]);
+  for (int r = r0; r < r1; r += 2 * DEEP) {
+    fetch(r + DEEP, d[1], zz[1]);
+    work(r, d[0], zz[0]);
+    fetch(r + 2 * DEEP, d[0], zz[0]);
+    work(r + DEEP, d[1], zz[1]);
   }
 }
 
-// Largest |e| of the tensor, and the column sums of every block's rows.  Bound: HBM (dout and z are read once here; the
-// rounding pass finds what fits of them in L2).
+// How the blocks of the error passes are dealt: `strips` column strips times row blocks of `rows` rows, then what else a pass
+// does beside them.
+struct ErrorGrid { int strips, rows, main; };
+
+// Largest |e| of the tensor, and the column sums of every block's rows; beside them, operands whose rows have to be padded for
+// the multiplies.  Bound: HBM (dout and z are read once here; the rounding pass finds what fits of them in L2).
 template <int T, int VEC, int ACT>
 __global__ void __launch_bounds__(ERR_THREADS)
-error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int M, int N, int rows) {
-  niti_enter(dout, z);
-  const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = (int)blockIdx.y * rows, r1 = min(r0 + rows, M);
-  if (next && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) niti_zero_header(next, (int)threadIdx.x);
+error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int M, int N, ErrorGrid g, PadJob pad0, PadJob pad1,
+                 unsigned pad0_blocks) {
+  niti_enter(dout, z, pad0.src, pad1.src);
+  if ((int)blockIdx.x >= g.main) {
+    const unsigned b = blockIdx.x - (unsigned)g.main, all = gridDim.x - (unsigned)g.main;
+    if (b < pad0_blocks) niti_pad_rows(pad0, b, pad0_blocks);
+    else niti_pad_rows(pad1, b - pad0_blocks, all - pad0_blocks);
+    return;
+  }
+  const int by = (int)blockIdx.x / g.strips, bx = (int)blockIdx.x - by * g.strips;
+  const int c = (bx * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * g.rows, r1 = min(r0 + g.rows, M);
+  if (next && blockIdx.x == 0 && threadIdx.x < 32) niti_zero_header(next, (int)threadIdx.x);
   float sum[VEC];
   float largest = 0.0f;
 #pragma unroll
@@ -607,7 +694,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
     });
     if (part) {
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) part[(long long)blockIdx.y * N + c + j] = sum[j];
+      for (int j = 0; j < VEC; ++j) part[(long long)by * N + c + j] = sum[j];
     }
   }
   const unsigned most = __reduce_max_sync(0xffffffffu, __float_as_uint(largest));
@@ -615,20 +702,27 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 }
 
 // e as payload with the exponent of its maximum, rows of `pitch` bytes.  The rows that the pass before read last come first.
+// Beside it, the bias gradient from that pass' column sums (of `nblk` row blocks).
 template <int T, int VEC, int ACT, bool PSR>
 __global__ void __launch_bounds__(ERR_THREADS)
-error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, int rows,
-                   int pitch) {
-  niti_enter(dout, z, hdr);
+error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, ErrorGrid g,
+                   int pitch, const float *part, float *dbias, int nblk) {
+  niti_enter(dout, z, hdr, part);
   const unsigned most = hdr->maxabs32;
   const int s = niti_exponent_of(most);
   const float scale = niti_payload_scale(niti_pow2(-s), PSR ? NITI_ROUND_PSR : NITI_ROUND_NEAREST);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
     *s_e = s;
     if (most >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
   }
-  const int by = (int)(gridDim.y - 1 - blockIdx.y);
-  const int c = ((int)blockIdx.x * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * rows, r1 = min(r0 + rows, M);
+  if ((int)blockIdx.x >= g.main) {
+    __shared__ float buf[16 * 33];
+    if (N % 4 == 0) niti_column_sums<4, 16>(part, dbias, nblk, N, (int)blockIdx.x - g.main, buf);
+    else niti_column_sums<1, 4>(part, dbias, nblk, N, (int)blockIdx.x - g.main, buf);
+    return;
+  }
+  const int b = g.main - 1 - (int)blockIdx.x, by = b / g.strips, bx = b - by * g.strips;
+  const int c = (bx * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * g.rows, r1 = min(r0 + g.rows, M);
   if (c >= N) return;
   error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
     niti_store_payload<VEC, PSR>(e8, (long long)r * pitch + c, e, scale);
@@ -647,7 +741,7 @@ int error_blocks(long long M, long long N) {
 
 }  // namespace
 
-int niti_launch_pad_pitch(niti_ctx *ctx, cudaStream_t st, const int8_t *src, int8_t *dst, long long rows, int n, int pitch);
+int niti_launch_pad_pitch2(niti_ctx *ctx, cudaStream_t st, const PadJob &a, const PadJob &b);
 int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C);
 
 size_t niti_linear_act_ws_bytes(int op, long long M, long long N, long long K) {
@@ -695,14 +789,15 @@ extern "C" int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a,
   int *slabs = (int *)(pad + pad_bytes(M, K) + pad_bytes(N, K));
   const int pitch = (int)pitch16(K);
   if (pitch != K) {
-    if ((rc = niti_launch_pad_pitch(ctx, st, a, pad, M, K, pitch)) != NITI_OK) return rc;
-    if ((rc = niti_launch_pad_pitch(ctx, st, w, pad + pad_bytes(M, K), N, K, pitch)) != NITI_OK) return rc;
+    rc = niti_launch_pad_pitch2(ctx, st, PadJob{a, pad, M, K, pitch}, PadJob{w, pad + pad_bytes(M, K), N, K, pitch});
+    if (rc != NITI_OK) return rc;
     a = pad;
     w = pad + pad_bytes(M, K);
   }
   WsHeader *hdr = niti_take_header(ctx, st, ws), *next = nullptr;
   if ((rc = niti_clear(ctx, st, nullptr, 0, &next)) != NITI_OK) return rc;
-  rc = niti_linear_gemm(ctx, st, GK_FC_FWD, a, pitch, w, pitch, M, N, K, e, type, slabs, niti_split_max(hdr), next);
+  const LinearMultiply x = {GK_FC_FWD, type, a, w, pitch, pitch, M, N, K, e};
+  rc = run_multiplies<1>(ctx, st, &x, slabs, niti_split_max(hdr), next);
   if (rc == NITI_OK) niti_header_passed_on(ctx, next);
   return rc;
 }
@@ -735,19 +830,29 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
   int8_t *e8 = (int8_t *)part + up256((size_t)nblk * (size_t)N * 4);
   WsHeader *hdr = niti_take_header(ctx, st, ws), *next = nullptr;
   if ((rc = niti_clear(ctx, st, nullptr, 0, &next)) != NITI_OK) return rc;
-  const int rows = (M + nblk - 1) / nblk;
+  const int rows = (M + nblk - 1) / nblk, blocks = (M + rows - 1) / rows;
   const int v16 = 16 / (int)es;
   const bool vec = N % v16 == 0 && (((uintptr_t)dout | (uintptr_t)z) & 15) == 0;
+  // operands with padded rows, copied beside the first pass
+  const bool pads = pitch != K;
+  const PadJob job_w = {w, pad_w, N, K, pitch}, job_a = {a, pad_a, M, K, pitch};
+  const unsigned pad0 = pads && dx ? niti_pad_blocks(job_w, ERR_THREADS, 4LL * ctx->sm_count) : 0;
+  const unsigned pad1 = pads && dw ? niti_pad_blocks(job_a, ERR_THREADS, 4LL * ctx->sm_count) : 0;
   auto passes_as = [&](auto tc, auto vc, auto ac) -> int {
     constexpr int T = decltype(tc)::value, VEC = decltype(vc)::value, ACT = decltype(ac)::value;
-    const dim3 grid((unsigned)((N + ERR_THREADS * VEC - 1) / (ERR_THREADS * VEC)), (unsigned)((M + rows - 1) / rows));
-    NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_max_kernel<T, VEC, ACT>, dout, z, dbias ? part : (float *)nullptr, hdr, next, M, N, rows));
+    ErrorGrid g;
+    g.strips = (N + ERR_THREADS * VEC - 1) / (ERR_THREADS * VEC);
+    g.rows = rows;
+    g.main = g.strips * blocks;
+    NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)g.main + pad0 + pad1, ERR_THREADS, 0, error_max_kernel<T, VEC, ACT>, dout, z,
+                                   dbias ? part : (float *)nullptr, hdr, next, M, N, g, job_w, job_a, pad0));
     ctx->launches++;
     niti_header_passed_on(ctx, next);
-    if (!dx && !dw) return NITI_OK;
+    if (!dx && !dw) return niti_launch_column_sums(ctx, st, part, dbias, blocks, N);
     auto second = [&](auto psr) -> int {
-      NITI_CUDA_TRY(ctx, niti_launch(st, grid, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT, decltype(psr)::value>, dout, z, e8, s_e,
-                                     (const WsHeader *)hdr, ctx->d_status, M, N, rows, pitch_e));
+      const unsigned extra = dbias ? (unsigned)((N + 31) / 32) : 0u;
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)g.main + extra, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT, decltype(psr)::value>, dout, z, e8, s_e,
+                                     (const WsHeader *)hdr, ctx->d_status, M, N, g, pitch_e, (const float *)part, dbias, blocks));
       ctx->launches++;
       return NITI_OK;
     };
@@ -771,27 +876,10 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
   };
   rc = type == NITI_F32 ? by_type(std::integral_constant<int, NITI_F32>{}) : type == NITI_BF16 ? by_type(std::integral_constant<int, NITI_BF16>{})
                         : by_type(std::integral_constant<int, NITI_F16>{});
-  if (rc != NITI_OK) return rc;
-  if (dbias && (rc = niti_launch_column_sums(ctx, st, part, dbias, (M + rows - 1) / rows, N)) != NITI_OK) return rc;
-  if (dx) {
-    const int8_t *q = w;
-    if (pitch != K) {
-      if ((rc = niti_launch_pad_pitch(ctx, st, w, pad_w, N, K, pitch)) != NITI_OK) return rc;
-      q = pad_w;
-    }
-    const LinearEpilogue e = {s_e, s_w, nullptr, nullptr, dx, nullptr, 0, NITI_ACT_NONE};
-    if ((rc = niti_linear_gemm(ctx, st, GK_FC_DGRAD, e8, pitch_e, q, pitch, M, K, N, e, type, slabs, niti_split_max(hdr), nullptr)) != NITI_OK) return rc;
-  }
-  if (dw) {
-    const int8_t *q = a;
-    if (pitch != K) {
-      if ((rc = niti_launch_pad_pitch(ctx, st, a, pad_a, M, K, pitch)) != NITI_OK) return rc;
-      q = pad_a;
-    }
-    const LinearEpilogue e = {s_e, s_a, nullptr, nullptr, dw, nullptr, 0, NITI_ACT_NONE};
-    if ((rc = niti_linear_gemm(ctx, st, GK_FC_WGRAD, e8, pitch_e, q, pitch, N, K, M, e, dw_type, slabs, niti_split_max(hdr) + NITI_LINEAR_COUNTERS,
-                               nullptr)) != NITI_OK)
-      return rc;
-  }
-  return NITI_OK;
+  if (rc != NITI_OK || (!dx && !dw)) return rc;
+  const LinearEpilogue e_x = {s_e, s_w, nullptr, nullptr, dx, nullptr, 0, NITI_ACT_NONE}, e_w = {s_e, s_a, nullptr, nullptr, dw, nullptr, 0, NITI_ACT_NONE};
+  const LinearMultiply both[2] = {{GK_FC_DGRAD, type, e8, pads ? pad_w : w, pitch_e, pitch, M, K, N, e_x},
+                                  {GK_FC_WGRAD, dw_type, e8, pads ? pad_a : a, pitch_e, pitch, N, K, M, e_w}};
+  unsigned *counters = niti_split_max(hdr);
+  return run_multiplies<2>(ctx, st, both, slabs, counters, nullptr);          // (one without an output has no items)
 }

@@ -14,12 +14,16 @@ struct LinearEpilogue {
 
 // Contractions are split only where all shares run at once, so that their sums take at most a tile of 128 x 256 words an SM.
 #define NITI_LINEAR_MAX_SMS 160
-// One multiply on the tensor cores; operands with 16-byte aligned rows of pitch ld0, ld1.  kind: GK_FC_FWD (A [gm][gk], B
-// [gn][gk]), GK_FC_DGRAD (A [gm][gk], B [gk][gn]) or GK_FC_WGRAD (A [gk][gm], B [gk][gn]).  counters: NITI_LINEAR_COUNTERS
-// zeroed words; next: a header to be zeroed for a later call, or null.
+// A multiply on the tensor cores; operands with 16-byte aligned rows of pitch ld0, ld1.  kind: GK_FC_FWD (A [gm][gk], B
+// [gn][gk]), GK_FC_DGRAD (A [gm][gk], B [gk][gn]) or GK_FC_WGRAD (A [gk][gm], B [gk][gn]).  e.out null: not wanted.
+struct LinearMultiply {
+  int kind, type;
+  const int8_t *p0, *p1;
+  long long ld0, ld1, gm, gn, gk;
+  LinearEpilogue e;
+};
+// Words of a zeroed header that count the arrivals of a multiply's split tiles.
 #define NITI_LINEAR_COUNTERS 320
 // The forward multiply of at most NITI_LINEAR_ROWS rows: streams the weights, in the caller's layout whatever K is.
 #define NITI_LINEAR_ROWS 32
 int niti_linear_rows(niti_ctx *ctx, cudaStream_t st, const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue &e, int type);
-int niti_linear_gemm(niti_ctx *ctx, cudaStream_t st, int kind, const int8_t *p0, long long ld0, const int8_t *p1, long long ld1, long long gm,
-                     long long gn, long long gk, const LinearEpilogue &e, int type, int *slabs, unsigned *counters, WsHeader *next);

@@ -3,6 +3,7 @@
 // taken.
 #include "niti_div.h"
 #include "niti_float.cuh"
+#include "niti_sums.cuh"
 #include <type_traits>
 
 namespace {
@@ -358,39 +359,12 @@ norm_wide_gain_kernel(const void *dy, const void *h, const float *rstd, float *p
   part[(long long)blockIdx.y * C + c] = sum;
 }
 
-// dst[c] = sum over the rows of part[n][C], in a fixed order: 32 columns a block, 32 threads for every W of them (bound: the
-// latency of a few loads; with eight threads a column 296 rows of 4096 took 6.4 us).
 template <int W>
 __global__ void __launch_bounds__(256 * 4 / W)
 column_sum_kernel(const float *part, float *dst, int n, int C) {
-  constexpr int PER = 32 / W;                         // threads side by side
-  __shared__ float buf[32][33];
+  __shared__ float buf[32 * 33];
   niti_enter(part);
-  const int tx = (int)threadIdx.x % PER, ty = (int)threadIdx.x / PER;
-  const int c = (int)blockIdx.x * 32 + tx * W;
-  float sum[W];
-#pragma unroll
-  for (int j = 0; j < W; ++j) sum[j] = 0.0f;
-  if (c < C) {
-#pragma unroll 8
-    for (int i = ty; i < n; i += 32) {
-      if constexpr (W == 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(part + (long long)i * C + c);
-        sum[0] += v.x; sum[1] += v.y; sum[2] += v.z; sum[3] += v.w;
-      } else {
-        sum[0] += part[(long long)i * C + c];
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < W; ++j) buf[ty][tx * W + j] = sum[j];
-  __syncthreads();
-  if (threadIdx.x < 32 && (int)blockIdx.x * 32 + (int)threadIdx.x < C) {
-    float all = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 32; ++k) all += buf[k][threadIdx.x];
-    dst[blockIdx.x * 32 + threadIdx.x] = all;
-  }
+  niti_column_sums<W, 32>(part, dst, n, C, (int)blockIdx.x, buf);
 }
 
 __device__ __forceinline__ float exponent_scale(int e) {
