@@ -446,8 +446,7 @@ int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, cons
  * comes straight from a 16-bit type has too few of them, and calls that would round such values refuse it.
  * Exponents go to s[M], one per row, with row_exponents != 0 (a row is then independent of the others: serving), else to
  * s[0], one for the tensor (what the backward multiplies can take out of their sums: training).
- * An infinity or NaN raises NITI_DEV_NONFINITE; its row's (tensor's) exponent is then 121, NaN becomes payload 0 and an
- * infinity +-127.
+ * An infinity or NaN raises NITI_DEV_NONFINITE; its row's (tensor's) exponent is then 121, its payload +-127.
  *
  * Root-mean-square norm:  h = x + residual (rounded to `type`; without a residual h is x and not written),
  *   r = 1 / sqrt(mean_c h^2 + eps),  y = round(h r gain).

@@ -145,25 +145,27 @@ __device__ __forceinline__ float niti_absmax(float m, float x) {
 
 // Magnitudes in units of the result to whole numbers, at most 127.  Pseudo-stochastic: the 16 fraction bits are split into
 // halves, rounded up where the top half is larger than the bottom half (Algorithm 3 with bp = 16; the sum carries into bit
-// 16 exactly then).  To nearest: half up, as everywhere in the library.  (Conversions saturate, and turn NaN into 0.)
+// 16 exactly then).  To nearest: half up, as everywhere in the library.
 // `scale` is that of niti_payload_scale(): in the first case results come in bits 16 .. 22, so that the multiplication
-// that scales also makes room for the fraction.
+// that scales also makes room for the fraction.  The whole part comes out of an addition of 2^23 that rounds towards zero (a
+// conversion instruction takes a slot of the pipe of exponentials and reciprocals, a quarter as wide); the exponent that it
+// leaves in the word does not reach bit 23.  NaN becomes 127.
 __device__ __forceinline__ float niti_payload_scale(float units, int round_mode) {
   return round_mode == NITI_ROUND_PSR ? units * 65536.0f : units;
 }
 template <bool PSR>
 __device__ __forceinline__ unsigned niti_unit_mag(float x, float scale) {
   if constexpr (PSR) {
-    const unsigned v = min(__float2uint_rz(fabsf(x) * scale), 127u << 16);
+    const unsigned v = __float_as_uint(__fadd_rz(fminf(fabsf(x) * scale, 127.0f * 65536.0f), 8388608.0f));
     return v + (~v & 255u) * 256u;
   } else {
-    return min(__float2uint_rz(fmaf(fabsf(x), scale, 0.5f)), 127u);
+    return __float_as_uint(__fadd_rz(fminf(fmaf(fabsf(x), scale, 0.5f), 127.0f), 8388608.0f));
   }
 }
 // (of 127 << 16 the sum is 127 << 16 | 0xff00: the same byte)
 template <bool PSR>
 __device__ __forceinline__ int niti_payload(float x, float scale) {
-  const int q = (int)(PSR ? niti_unit_mag<PSR>(x, scale) >> 16 : niti_unit_mag<PSR>(x, scale));
+  const int q = (int)((PSR ? niti_unit_mag<PSR>(x, scale) >> 16 : niti_unit_mag<PSR>(x, scale)) & 127u);
   return x < 0.0f ? -q : q;
 }
 // Four payloads in a word: magnitudes gathered by byte permutes, signs as bytes of zeros or ones (a permute with sign

@@ -733,9 +733,10 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 long long pitch16(long long n) { return (n + 15) / 16 * 16; }
 size_t pad_bytes(long long rows, long long width) { return width % 16 ? up256((size_t)rows * (size_t)pitch16(width)) : 0; }
 
-// Row blocks of the error passes: about 1024 blocks of 1024 columns in all, of 16 rows or more.
+// Row blocks of the error passes: as many blocks of 1024 columns as run at once (eight on each of 148 SMs), of four rows or
+// more.
 int error_blocks(long long M, long long N) {
-  const long long strips = (N + 1023) / 1024, most = strips >= 1024 ? 1 : 1024 / strips, want = (M + 15) / 16;
+  const long long strips = (N + 1023) / 1024, most = strips >= 1184 ? 1 : 1184 / strips, want = (M + 3) / 4;
   return (int)(want < most ? want : most);
 }
 
