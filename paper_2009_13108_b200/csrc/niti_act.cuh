@@ -18,26 +18,65 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// The normal distribution's tail for a = |z|: 1 - Phi(a) = t (a1 + t (a2 + ...)) exp(-a^2 / 2) / 2 with t = 1 / (1 + p a / sqrt 2),
-// Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, of Phi half of that).  g receives exp(-a^2 / 2).
-__device__ __forceinline__ float normal_tail(float z, float &g) {
-  const float t = fast_reciprocal(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-  g = fast_exp2(z * -0.72134752f * z);
-  float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-  q = fmaf(t, q, 0.5f * 1.421413741f);
-  q = fmaf(t, q, 0.5f * -0.284496736f);
-  q = fmaf(t, q, 0.5f * 0.254829592f);
-  return q * t * g;
+// Two float32 values for the packed instructions (each a multiply-add, multiplication or addition of both).
+struct F2 {
+  unsigned long long v;
+  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit F2(float a) : F2(a, a) {}
+  __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+};
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r = c;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r = a;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r = a;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+
+// Phi of two values, and exp(-z^2 / 2).  For a = |z|: 1 - Phi(a) = t (a1 + t (a2 + ...)) exp(-a^2 / 2) / 2 with t = 1 / (1 + p a /
+// sqrt 2), Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, of Phi half of that).  Phi(z) = 1/2 + sign(z) (1/2 - that).
+__device__ __forceinline__ F2 normal_cdf2(float z0, float z1, F2 z, F2 &g) {
+  float d0, d1, x0, x1;
+  fma2(F2(fabsf(z0), fabsf(z1)), F2(0.3275911f * 0.70710678f), F2(1.0f)).get(d0, d1);
+  mul2(mul2(z, F2(-0.72134752f)), z).get(x0, x1);
+  const F2 t(fast_reciprocal(d0), fast_reciprocal(d1));
+  g = F2(fast_exp2(x0), fast_exp2(x1));
+  F2 q = fma2(t, F2(-0.5f * 1.061405429f), F2(0.5f * 1.453152027f));
+  q = fma2(t, q, F2(-0.5f * 1.421413741f));
+  q = fma2(t, q, F2(0.5f * 0.284496736f));
+  q = fma2(t, q, F2(-0.5f * 0.254829592f));
+  float h0, h1;                                    // 1/2 - tail
+  fma2(mul2(q, t), g, F2(0.5f)).get(h0, h1);
+  return add2(F2(copysignf(h0, z0), copysignf(h1, z1)), F2(0.5f));
+}
+__device__ __forceinline__ F2 gelu2(float z0, float z1) {
+  const F2 z(z0, z1);
+  F2 g(0.0f);
+  return mul2(z, normal_cdf2(z0, z1, z, g));
+}
+__device__ __forceinline__ F2 gelu_slope2(float z0, float z1) {
+  const F2 z(z0, z1);
+  F2 g(0.0f);
+  const F2 cdf = normal_cdf2(z0, z1, z, g);
+  return fma2(mul2(z, F2(0.3989422804f)), g, cdf);
 }
 __device__ __forceinline__ float gelu(float z) {
-  float g;
-  const float tail = normal_tail(z, g);
-  return z * (z < 0.0f ? tail : 1.0f - tail);
+  float a, b;
+  gelu2(z, z).get(a, b);
+  return a;
 }
 __device__ __forceinline__ float gelu_slope(float z) {
-  float g;
-  const float tail = normal_tail(z, g);
-  return fmaf(z * 0.3989422804f, g, z < 0.0f ? tail : 1.0f - tail);
+  float a, b;
+  gelu_slope2(z, z).get(a, b);
+  return a;
 }
 __device__ __forceinline__ float sigmoid(float z) { return fast_reciprocal(1.0f + fast_exp2(z * -1.44269504f)); }
 __device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
@@ -61,6 +100,18 @@ __device__ __forceinline__ float act_slope(float z, int act) {
     default: return 1.0f;
   }
 }
+// e = d act'(z) for a vector
+template <int ACT, int N>
+__device__ __forceinline__ void act_backward(const float (&d)[N], const float (&z)[N], float (&e)[N]) {
+  if constexpr (ACT == NITI_ACT_GELU && N % 2 == 0) {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) mul2(F2(d[j], d[j + 1]), gelu_slope2(z[j], z[j + 1])).get(e[j], e[j + 1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) e[j] = d[j] * act_slope(z[j], ACT);
+  }
+}
+// (N even)
 template <int N>
 __device__ __forceinline__ void act_all(float (&x)[N], int act) {
   switch (act) {
@@ -70,7 +121,7 @@ __device__ __forceinline__ void act_all(float (&x)[N], int act) {
       break;
     case NITI_ACT_GELU:
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = gelu(x[j]);
+      for (int j = 0; j + 1 < N; j += 2) gelu2(x[j], x[j + 1]).get(x[j], x[j + 1]);
       break;
     case NITI_ACT_SILU:
 #pragma unroll

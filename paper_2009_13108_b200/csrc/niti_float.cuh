@@ -20,11 +20,12 @@ struct Pack {
   static constexpr int WORDS = (BYTES + 3) / 4;
   unsigned w[WORDS];
 
-  // (streaming: every element of these tensors is read once per launch)
+  // KEEP: the next launch reads it again (else marked as the first to leave L2)
+  template <bool KEEP = false>
   __device__ __forceinline__ void load(const void *p, long long i) {
     const char *q = reinterpret_cast<const char *>(p) + i * (long long)sizeof(typename FloatOf<T>::type);
     if constexpr (BYTES == 16) {
-      const uint4 v = __ldcs(reinterpret_cast<const uint4 *>(q));
+      const uint4 v = KEEP ? __ldcg(reinterpret_cast<const uint4 *>(q)) : __ldcs(reinterpret_cast<const uint4 *>(q));
       w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
     } else if constexpr (BYTES == 4) {
       w[0] = *reinterpret_cast<const unsigned *>(q);

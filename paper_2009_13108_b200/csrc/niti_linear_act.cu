@@ -629,7 +629,7 @@ constexpr unsigned INF_BITS = 0x7f800000u;
 
 // e = dout act'(z) of a block's rows and columns, a thread on the same VEC columns in every row; two rows at work and two on
 // their way.
-template <int T, int VEC, int ACT, typename F>
+template <int T, int VEC, int ACT, bool KEEP, typename F>
 __device__ __forceinline__ void error_rows(const void *dout, const void *z, int N, int r0, int r1, int c, F take) {
   constexpr int DEEP = 2;
   Pack<T, VEC> d[2][DEEP], zz[2][DEEP];
@@ -637,8 +637,8 @@ __device__ __forceinline__ void error_rows(const void *dout, const void *z, int 
 #pragma unroll
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
-        dd[k].load(dout, (long long)(r + k) * N + c);
-        if (ACT != NITI_ACT_NONE) zd[k].load(z, (long long)(r + k) * N + c);
+        dd[k].template load<KEEP>(dout, (long long)(r + k) * N + c);
+        if (ACT != NITI_ACT_NONE) zd[k].template load<KEEP>(z, (long long)(r + k) * N + c);
       }
   };
   auto work = [&](int r, const Pack<T, VEC> (&dd)[DEEP], const Pack<T, VEC> (&zd)[DEEP]) {
@@ -646,8 +646,18 @@ __device__ __forceinline__ void error_rows(const void *dout, const void *z, int 
     for (int k = 0; k < DEEP; ++k)
       if (r + k < r1) {
         float e[VEC];
+        if constexpr (ACT == NITI_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) e[j] = ACT == NITI_ACT_NONE ? dd[k].get(j) : dd[k].get(j) * act_slope(zd[k].get(j), ACT);
+          for (int j = 0; j < VEC; ++j) e[j] = dd[k].get(j);
+        } else {
+          float dv[VEC], zv[VEC];
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) {
+            dv[j] = dd[k].get(j);
+            zv[j] = zd[k].get(j);
+          }
+          act_backward<ACT>(dv, zv, e);
+        }
         take(r + k, e);
       }
   };
@@ -685,7 +695,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 #pragma unroll
   for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
   if (c < N) {
-    error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int, const float (&e)[VEC]) {
+    error_rows<T, VEC, ACT, true>(dout, z, N, r0, r1, c, [&](int, const float (&e)[VEC]) {
 #pragma unroll
       for (int j = 0; j < VEC; ++j) {
         sum[j] += e[j];
@@ -724,7 +734,7 @@ error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, co
   const int b = g.main - 1 - (int)blockIdx.x, by = b / g.strips, bx = b - by * g.strips;
   const int c = (bx * ERR_THREADS + (int)threadIdx.x) * VEC, r0 = by * g.rows, r1 = min(r0 + g.rows, M);
   if (c >= N) return;
-  error_rows<T, VEC, ACT>(dout, z, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
+  error_rows<T, VEC, ACT, false>(dout, z, N, r0, r1, c, [&](int r, const float (&e)[VEC]) {
     niti_store_payload<VEC, PSR>(e8, (long long)r * pitch + c, e, scale);
   });
 }

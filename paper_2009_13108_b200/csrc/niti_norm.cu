@@ -82,7 +82,7 @@ norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int
 #pragma unroll
     for (int v = 0; v < NV; ++v)
       if (in[v] && row < sh.M) {
-        px[v].load(x, at + (long long)v * sh.tpr * VEC);
+        px[v].template load<SHARED>(x, at + (long long)v * sh.tpr * VEC);
         if (NORM && res) pr[v].load(res, at + (long long)v * sh.tpr * VEC);
       }
   };
