@@ -8,6 +8,13 @@
 
 #include "../../include/niti.h"
 
+// How the float-epilogue multiplies of earlier sizes were tiled (niti_linear_act.cu).
+#define NITI_LINEAR_PLANS 128
+struct NitiLinearPlan {
+  long long key[4];
+  int bn, splits;           // bn 0: empty
+  double cycles;
+};
 struct niti_ctx {
   int device;
   int sm_count;
@@ -61,6 +68,7 @@ struct niti_ctx {
   size_t smem_optin;
   bool adamw_ready[4];      // shared-memory limits of the optimizer's instances are set
   bool linear_ready[36];    // attributes of the instances of the float-epilogue kernel are set
+  NitiLinearPlan linear_plans[NITI_LINEAR_PLANS];
   int linear_pairs;         // CTA pairs of it that run at once (0: not asked yet)
   int small_ready;          // attributes of the small-multiply kernel are set
   unsigned patience;        // cycles that the blocks of a launch wait for each other (NITI_PATIENCE; 0: test switch)

@@ -13,7 +13,7 @@ namespace {
 
 constexpr int BM = 128;                            // rows of a tile = TMEM lanes
 constexpr int PROD_WARPS = 3, MMA_WARP = 3, EPI_WARP0 = 4;
-constexpr int EPI_WARPS = 8;
+constexpr int EPI_WARPS = 16;
 constexpr int THREADS = 32 * (EPI_WARP0 + EPI_WARPS);
 constexpr int MAX_STAGES = 8, MAX_TBUF = 4;
 constexpr int STG_FLOATS = 32 * 33;                // a warp's buffer for rows that are not whole, aligned vectors
@@ -414,6 +414,22 @@ Choice choose(const niti_ctx *ctx, const LinearMultiply &x, int ctas, long long 
   return best;
 }
 
+// The same for the sizes of an earlier call: the search takes longer than a small multiply.
+Choice chosen(niti_ctx *ctx, const LinearMultiply &x, int ctas, long long units, bool direct) {
+  const long long key[4] = {x.gm, x.gn, x.gk, ((x.kind * 2LL + direct) * 2 + ctas - 1) * 1024 + units};
+  unsigned long long h = 0;
+  for (int i = 0; i < 4; ++i) h = (h ^ (unsigned long long)key[i]) * 0x9E3779B97F4A7C15ull;
+  NitiLinearPlan &e = ctx->linear_plans[(h >> 32) % NITI_LINEAR_PLANS];
+  if (memcmp(e.key, key, sizeof(key)) != 0 || !e.bn) {
+    const Choice c = choose(ctx, x, ctas, units, direct ? 20.0 : 40.0);
+    memcpy(e.key, key, sizeof(key));
+    e.bn = c.bn;
+    e.splits = c.splits;
+    e.cycles = c.cycles;
+  }
+  return Choice{e.bn, e.splits, e.cycles};
+}
+
 template <int N, int CTAS, int T0, int T1>
 int set_up(niti_ctx *ctx) {
   // (per device and instance, the same value in every context: see niti_ctx::smem_optin)
@@ -558,7 +574,7 @@ int run_multiplies(niti_ctx *ctx, cudaStream_t st, const LinearMultiply *x, int 
     for (int i = 0; i < N; ++i) {
       if (!x[i].e.out) continue;
       const long long units = (ctas == 2 ? ctx->linear_pairs : ctx->sm_count) / wanted;
-      c[ctas - 1][i] = choose(ctx, x[i], ctas, units < 1 ? 1 : units, direct_rows(x[i]) ? 20.0 : 40.0);
+      c[ctas - 1][i] = chosen(ctx, x[i], ctas, units < 1 ? 1 : units, direct_rows(x[i]));
       if (c[ctas - 1][i].cycles > cycles[ctas - 1]) cycles[ctas - 1] = c[ctas - 1][i].cycles;
       if (ctas == 2 && x[i].gm <= BM) cycles[1] = 1e300;
     }
