@@ -353,7 +353,9 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   }
   Step st;
   // 1 - b^t without its cancellation
-  const float lr = fmaxf(hy.lr / -expm1f((float)t_step * hy.log_b1), 1e-37f);        // (0: a step of nothing)
+  // (a learning rate of 0 becomes a step of nothing; with the bounds that the call puts on lr and eps every denominator is
+  // finite and not 0, so that an element without a gradient does not become 0 / 0 or 0 times infinity)
+  const float lr = fmaxf(hy.lr / -expm1f((float)t_step * hy.log_b1), 1e-30f);
   st.den_r = -rsqrtf(-expm1f((float)t_step * hy.log_b2)) / lr;
   st.den_1 = -hy.eps / lr;
   st.gs = grad_scale ? *grad_scale : 1.0f;
@@ -486,12 +488,12 @@ extern "C" int niti_adamw(niti_ctx *ctx, void *stream, const niti_adamw_tensor *
                           double beta1, double beta2, double eps, const float *grad_scale) {
   if (!ctx) return NITI_ERR_ARG;
   if (n < 0 || (n > 0 && !t) || !step || ((uintptr_t)step & 3) || ((uintptr_t)grad_scale & 3) || (state_bits != 8 && state_bits != 32) ||
-      !(lr >= 0.0) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps > 0.0))
+      !(lr >= 0.0 && lr <= 1e6) || !(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(eps >= 1e-20 && eps <= 1e6))
     return niti_fail(ctx, NITI_ERR_ARG, "niti_adamw: bad argument");
   const bool eight = state_bits == 8;
   for (int i = 0; i < n; ++i) {
     const niti_adamw_tensor &a = t[i];
-    if (a.n < 0 || !niti_type_ok(a.g_type) || !(a.weight_decay >= 0.0f))
+    if (a.n < 0 || !niti_type_ok(a.g_type) || !(a.weight_decay >= 0.0f && a.weight_decay <= 1e6f))
       return niti_fail(ctx, NITI_ERR_ARG, "niti_adamw: bad argument (size, gradient type or weight decay of a tensor)");
     if (a.n == 0) continue;
     const uintptr_t words = (uintptr_t)a.p | (uintptr_t)a.s_w | (eight ? 0 : (uintptr_t)a.m | (uintptr_t)a.v);

@@ -549,7 +549,7 @@ static int norm_args(niti_ctx *ctx, const char *name, int type, int M, int C, vo
     snprintf(ctx->err, sizeof(ctx->err), "%s: bad argument (type, or a size that is not positive)", name);
     return NITI_ERR_ARG;
   }
-  if (M > (1 << 30)) return niti_fail(ctx, NITI_ERR_SHAPE, "more than 2^30 rows");            // (row counters have 32 bits)
+  if (M > (1 << 30) || C > (1 << 30)) return niti_fail(ctx, NITI_ERR_SHAPE, "more than 2^30 rows or columns");    // (32-bit counters)
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < niti_norm_ws_bytes(op, M, C))
     return niti_fail(ctx, NITI_ERR_WORKSPACE, "workspace missing, misaligned or too small");
   return NITI_OK;

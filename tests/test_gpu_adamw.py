@@ -71,8 +71,8 @@ SIZES = [[1], [255, 256, 257], [1000, 8, 70001, 3], [5] * 40, [300 + 17 * i for 
 @pytest.mark.parametrize("gtype", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("w8", [False, True])
-def test_one_step(niti, sizes, gtype, bits, w8):
-    pr = _problem(sizes, bits, gtype, w8)
+def test_one_step(niti, sizes, gtype, bits, w8, pr=None):
+    pr = pr or _problem(sizes, bits, gtype, w8)
     t = 7
     want = [_expected(pr, i, bits, t) for i in range(len(sizes))]
     niti.adamw(_plan(niti, pr), torch.full((1,), t, dtype=torch.int32, device="cuda"), LR, (B1, B2), EPS)
@@ -88,6 +88,32 @@ def test_one_step(niti, sizes, gtype, bits, w8):
             u = np.abs(got) * 2.0 ** -int(pr["s_w"][i])          # (of the stored weight: exact)
             assert np.array_equal(_np(pr["w8"][i]), np.sign(got) * np.minimum(np.floor(u + 0.5), 127))
     assert niti.check() == 0
+
+
+def test_many_chunks(niti):
+    """Enough elements that a CTA takes several chunks in a row and stores their exponents together; the tensors end inside
+    chunks, and their exponents start on no particular boundary."""
+    sizes = [9_000_001, 300, 5_500_123, 2_100_000]
+    pr = _problem(sizes, 8, torch.bfloat16, True)
+    whole = torch.zeros(sum(x.numel() for x in pr["s_m"]) + 3, dtype=torch.int8, device="cuda")
+    at = 3
+    for i, e in enumerate(pr["s_m"]):
+        whole[at:at + e.numel()] = e
+        pr["s_m"][i] = whole[at:at + e.numel()]
+        at += e.numel()
+    before = pr["p"][1].clone()
+    test_one_step(niti, sizes, torch.bfloat16, 8, True, pr=pr)
+    assert not torch.equal(before, pr["p"][1]) and not whole[:3].any()
+
+
+def test_a_learning_rate_of_zero_changes_the_states_alone(niti):
+    for bits in (32, 8):
+        pr = _problem([5000], bits, torch.float32, False)
+        for k in ("g", "m", "v"):
+            pr[k][0][::2] = 0                     # (no gradient, no states)
+        p0, m0 = pr["p"][0].clone(), pr["m"][0].clone()
+        niti.adamw(_plan(niti, pr), torch.ones(1, dtype=torch.int32, device="cuda"), 0.0, (0.9, 0.99999), 1e-8)
+        assert torch.equal(pr["p"][0], p0) and not torch.equal(pr["m"][0], m0)
 
 
 def _check_codes(pr, i, m, v, m_slack, t):
