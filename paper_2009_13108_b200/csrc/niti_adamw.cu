@@ -35,7 +35,7 @@ struct List {
   Tensor t[MOST];
 };
 struct Hyper {
-  float lr, b1, b2, root_b2, c1, c2, eps;          // c = 1 - b
+  float lr, b1, b2, c1, c2, eps;                   // c = 1 - b
   float log_b1, log_b2;
   int group;                                       // chunks of a group
 };
@@ -46,11 +46,6 @@ __device__ __forceinline__ float load_grad(const void *g, int type, long long i)
   return __half2float(reinterpret_cast<const __half *>(g)[i]);
 }
 
-__device__ __forceinline__ float root(float x) {                      // (within a few steps of 2^-24; 0 for subnormal numbers)
-  float r;
-  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
 __device__ __forceinline__ float reciprocal(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -66,7 +61,7 @@ constexpr float LEAST_CODE = 1.1641532182693481e-10f;                   // 2^-9 
 template <bool SMALL>
 __device__ __forceinline__ unsigned draw_e4m3(float t, unsigned draw, unsigned sixteen) {
   unsigned b = __float_as_uint(t);
-  if (SMALL && t < LEAST_NORMAL) b = __float_as_uint(t + LEAST_NORMAL) - (8u << 20);
+  if (SMALL && t < LEAST_NORMAL) b = __float_as_uint(__fadd_rz(t, LEAST_NORMAL)) - (8u << 20);
   return draw * sixteen + b;
 }
 // The codes of four such words in one
@@ -94,11 +89,10 @@ __device__ __forceinline__ unsigned random_bits(unsigned index, unsigned key) {
 }
 
 struct Step {                                      // of this step and tensor
-  float b1, root_b2;                               // b1, sqrt(b2)
-  float c1, c2;                                    // (1 - b1) gs, (1 - b2) gs^2 for a gradient scale gs
   float den_r, den_1;                              // the step is m / (r den_r + den_1)
   float decay, gs, w_scale;
   unsigned key, sixteen;
+  bool scaled;                                     // gs is not simply 1
 };
 
 // A warp works on one block of 256 elements at a time, a lane on eight (two vectors of four, or every 32nd element).  8-bit
@@ -167,44 +161,48 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
       }
     }
   }
-  // the old states, already times b1 and b2
-  float k_m = st.b1, k_v = st.root_b2;
   if (EIGHT) {
-    k_m *= niti_pow2(s_m);
-    k_v *= niti_pow2(s_v);
+    const float k_m = niti_pow2(s_m), k_v = niti_pow2(s_v);
     values_e4m3(cm[0], *reinterpret_cast<float (*)[4]>(m));
     values_e4m3(cm[1], *reinterpret_cast<float (*)[4]>(m + 4));
     values_e4m3(cv[0], *reinterpret_cast<float (*)[4]>(v));
     values_e4m3(cv[1], *reinterpret_cast<float (*)[4]>(v + 4));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      m[j] *= k_m;
+      v[j] *= k_v;
+      v[j] *= v[j];
+    }
+  }
+  if (st.scaled) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] *= st.gs;
   }
   float worst = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) worst = niti_absmax(worst, g[j]);
-  const bool bad = !(worst * fabsf(st.gs) < __int_as_float(0x7f800000));
+  const bool bad = !(worst < __int_as_float(0x7f800000));
+  // The states are products and sums rounded one by one, without fused multiply-adds, and a correctly rounded root: a code
+  // follows from them alone, and so from the formulas, whatever computes them.
+  auto update = [&](int j) {
+    m[j] = __fadd_rn(__fmul_rn(hy.b1, m[j]), __fmul_rn(hy.c1, g[j]));
+    v[j] = __fadd_rn(__fmul_rn(hy.b2, v[j]), __fmul_rn(__fmul_rn(hy.c2, g[j]), g[j]));
+  };
+  auto move = [&](int j) { p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay); };
   if (!bad) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      m[j] = fmaf(m[j], k_m, st.c1 * g[j]);
-      const float old = EIGHT ? (v[j] * k_v) * (v[j] * k_v) : v[j] * hy.b2;
-      v[j] = fmaf(st.c2 * g[j], g[j], old);
-      r[j] = root(v[j]);
-      p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
+      update(j);
+      r[j] = __fsqrt_rn(v[j]);
+      move(j);
     }
   } else {                                         // (elements without a finite gradient keep what they have)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool ok = fabsf(g[j] * st.gs) < __int_as_float(0x7f800000);
-      const float old = EIGHT ? (v[j] * k_v) * (v[j] * k_v) : v[j] * hy.b2;
-      if (ok) {
-        m[j] = fmaf(m[j], k_m, st.c1 * g[j]);
-        v[j] = fmaf(st.c2 * g[j], g[j], old);
-      } else if (EIGHT) {
-        m[j] *= niti_pow2(s_m);
-        v[j] *= niti_pow2(s_v);
-        v[j] *= v[j];
-      }
-      r[j] = root(v[j]);
-      if (ok) p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
+      const bool ok = fabsf(g[j]) < __int_as_float(0x7f800000);
+      if (ok) update(j);
+      r[j] = __fsqrt_rn(v[j]);
+      if (ok) move(j);
     }
   }
   if (EIGHT) {
@@ -359,10 +357,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   st.den_r = -rsqrtf(-expm1f((float)t_step * hy.log_b2)) / lr;
   st.den_1 = -hy.eps / lr;
   st.gs = grad_scale ? *grad_scale : 1.0f;
-  st.b1 = hy.b1;
-  st.root_b2 = hy.root_b2;
-  st.c1 = hy.c1 * st.gs;
-  st.c2 = hy.c2 * st.gs * st.gs;
+  st.scaled = grad_scale != nullptr;
   st.key = (unsigned)t_step * 0x9E3779B9u;
   st.sixteen = 16u;
   asm volatile("" : "+r"(st.sixteen));
@@ -506,7 +501,6 @@ extern "C" int niti_adamw(niti_ctx *ctx, void *stream, const niti_adamw_tensor *
   hy.lr = (float)lr;
   hy.b1 = (float)beta1; hy.b2 = (float)beta2;
   hy.c1 = (float)(1.0 - beta1); hy.c2 = (float)(1.0 - beta2);
-  hy.root_b2 = (float)sqrt(beta2);
   hy.eps = (float)eps;
   // (b = 0: 1 - b^t is 1 for every t >= 1)
   hy.log_b1 = beta1 > 0.0 ? (float)log(beta1) : -1e30f;
