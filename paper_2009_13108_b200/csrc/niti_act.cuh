@@ -18,29 +18,6 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Two float32 values for the packed instructions (each a multiply-add, multiplication or addition of both).
-struct F2 {
-  unsigned long long v;
-  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ explicit F2(float a) : F2(a, a) {}
-  __device__ __forceinline__ void get(float &a, float &b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-};
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-  F2 r = c;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
-  F2 r = a;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 add2(F2 a, F2 b) {
-  F2 r = a;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-
 // Phi of two values, and exp(-z^2 / 2).  For a = |z|: 1 - Phi(a) = t (a1 + t (a2 + ...)) exp(-a^2 / 2) / 2 with t = 1 / (1 + p a /
 // sqrt 2), Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, of Phi half of that).  Phi(z) = 1/2 + sign(z) (1/2 - that).
 __device__ __forceinline__ F2 normal_cdf2(float z0, float z1, F2 z, F2 &g) {

@@ -11,11 +11,11 @@ constexpr int BLOCK = NITI_STATE_BLOCK;            // elements that share the ex
 static_assert(BLOCK == 256, "eight elements a lane");
 constexpr int WARPS = 8;
 constexpr int CHUNK = WARPS * BLOCK;               // elements that a CTA works on at a time
-constexpr int STAGES = 3;
+constexpr int STAGES = 2;
 constexpr int GROUP = 4;                           // chunks that a CTA takes in a row where there are many
 // bytes of a chunk in shared memory: weights, gradients (room for 32 bits), both states
 __host__ __device__ constexpr int stage_bytes(bool eight) { return CHUNK * (4 + 4 + (eight ? 2 : 8)); }
-__host__ __device__ constexpr int ctas_per_sm(bool eight) { return eight ? 3 : 2; }
+__host__ __device__ constexpr int ctas_per_sm(bool eight) { return eight ? 4 : 3; }
 constexpr int LIST_SMALL = 16, LIST_MOST = 256;    // tensors a launch takes (its parameters: 1.4 and 22 KB)
 
 struct Tensor {
@@ -50,6 +50,16 @@ __device__ __forceinline__ float reciprocal(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
+}
+// Roots of two values: the hardware's approximation r and a step of Heron's method, r + (v - r^2) / (2 r), whose residual a fused
+// multiply-add has exactly.  The step squares a relative error of 2^-22, so that what is left decides the rounding only within
+// 2^-20 of a step of a tie: as __fsqrt_rn() (compared by the tests), in half of its instructions.  0 stays 0.
+__device__ __forceinline__ F2 root2(float v0, float v1, F2 v) {
+  float r0, r1;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v0));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v1));
+  const F2 r(r0, r1), d = fma2(F2(-r0, -r1), r, v);
+  return fma2(d, F2(0.5f * reciprocal(fmaxf(r0, 1e-30f)), 0.5f * reciprocal(fmaxf(r1, 1e-30f))), r);
 }
 // In bits 20 .. 27, the code below a magnitude t < 256, given as t 2^-24, plus what 16 random bits (times 16: `sixteen` is 16
 // in a register, which keeps the multiply-add from becoming a shift and an addition on the busier integer pipe) carry into it.
@@ -168,10 +178,10 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
     values_e4m3(cv[0], *reinterpret_cast<float (*)[4]>(v));
     values_e4m3(cv[1], *reinterpret_cast<float (*)[4]>(v + 4));
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      m[j] *= k_m;
-      v[j] *= k_v;
-      v[j] *= v[j];
+    for (int j = 0; j < 8; j += 2) {
+      mul2(F2(m[j], m[j + 1]), F2(k_m)).get(m[j], m[j + 1]);
+      const F2 t = mul2(F2(v[j], v[j + 1]), F2(k_v));
+      mul2(t, t).get(v[j], v[j + 1]);
     }
   }
   if (st.scaled) {
@@ -183,18 +193,23 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
   for (int j = 0; j < 8; ++j) worst = niti_absmax(worst, g[j]);
   const bool bad = !(worst < __int_as_float(0x7f800000));
   // The states are products and sums rounded one by one, without fused multiply-adds, and a correctly rounded root: a code
-  // follows from them alone, and so from the formulas, whatever computes them.
+  // follows from them alone, and so from the formulas, whatever computes them.  (By single instructions: the assembler fuses
+  // packed multiplications and additions.)
   auto update = [&](int j) {
     m[j] = __fadd_rn(__fmul_rn(hy.b1, m[j]), __fmul_rn(hy.c1, g[j]));
     v[j] = __fadd_rn(__fmul_rn(hy.b2, v[j]), __fmul_rn(__fmul_rn(hy.c2, g[j]), g[j]));
   };
-  auto move = [&](int j) { p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay); };
   if (!bad) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < 8; j += 2) {
       update(j);
-      r[j] = __fsqrt_rn(v[j]);
-      move(j);
+      update(j + 1);
+      const F2 mm(m[j], m[j + 1]), vv(v[j], v[j + 1]);
+      const F2 rr = root2(v[j], v[j + 1], vv);
+      rr.get(r[j], r[j + 1]);
+      float d0, d1;
+      fma2(rr, F2(st.den_r), F2(st.den_1)).get(d0, d1);
+      fma2(mm, F2(reciprocal(d0), reciprocal(d1)), mul2(F2(p[j], p[j + 1]), F2(st.decay))).get(p[j], p[j + 1]);
     }
   } else {                                         // (elements without a finite gradient keep what they have)
 #pragma unroll
@@ -202,7 +217,7 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
       const bool ok = fabsf(g[j]) < __int_as_float(0x7f800000);
       if (ok) update(j);
       r[j] = __fsqrt_rn(v[j]);
-      if (ok) move(j);
+      if (ok) p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
     }
   }
   if (EIGHT) {

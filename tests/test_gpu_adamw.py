@@ -139,6 +139,37 @@ def _check_codes(pr, i, m, v, m_slack, t):
             assert sure.mean() > 0.8
 
 
+def test_codes_follow_from_float32_operations(niti):
+    """Every product and sum rounded to float32, the root correctly rounded: the codes are exactly those of numpy's float32."""
+    n, t = 1 << 20, 9
+    f = np.float32
+    pr = _problem([n], 8, torch.bfloat16, False, seed=5)
+    g = pr["g"][0].float().cpu().numpy()
+    m = decode_e4m3(pr["m"][0].cpu().numpy(), pr["s_m"][0].cpu().numpy()).astype(f)          # (exact)
+    r = decode_e4m3(pr["v"][0].cpu().numpy(), pr["s_v"][0].cpu().numpy()).astype(f)
+    m = f(B1) * m + f(1 - B1) * g
+    r = np.sqrt(f(B2) * (r * r) + f(1 - B2) * g * g)
+    assert m.dtype == r.dtype == f
+    niti.adamw(_plan(niti, pr), torch.full((1,), t, dtype=torch.int32, device="cuda"), LR, (B1, B2), EPS)
+    x = random_bits(n, t)
+    for name, value, draw, least in (("m", np.abs(m), x >> 16, 0), ("v", r, x & 65535, r > 0)):
+        s, code, frac, _ = split_e4m3(value.astype(np.float64))
+        want = np.maximum(code + ((np.floor(frac).astype(np.int64) + draw) >> 16), least)
+        assert np.array_equal(pr["s_" + name][0].cpu().numpy(), s)
+        got = pr[name][0].cpu().numpy().astype(np.int64)
+        assert np.array_equal(got & 127, want)
+    assert np.array_equal(pr["m"][0].cpu().numpy() >= 128, m < 0)
+
+
+def test_32_bit_states_are_numpys(niti):
+    n, f = 1 << 20, np.float32
+    pr = _problem([n], 32, torch.bfloat16, False, seed=6)
+    g, m, v = pr["g"][0].float().cpu().numpy(), pr["m"][0].cpu().numpy(), pr["v"][0].cpu().numpy()
+    niti.adamw(_plan(niti, pr), torch.ones(1, dtype=torch.int32, device="cuda"), LR, (B1, B2), EPS)
+    assert np.array_equal(pr["m"][0].cpu().numpy(), f(B1) * m + f(1 - B1) * g)
+    assert np.array_equal(pr["v"][0].cpu().numpy(), f(B2) * v + f(1 - B2) * g * g)
+
+
 def test_rounding_of_states_is_unbiased(niti):
     """bfloat16 gradients and short codes, whose weighted sums have repeating bits."""
     n = 1 << 20
