@@ -6,7 +6,6 @@
 
 namespace {
 
-constexpr int WARPS = 8;
 constexpr int DEEP = 4;                            // blocks of 64 contraction elements that a warp has in flight
 
 // 16 bytes of a row from element k on; elements from K on are zero.  ALIGNED: rows are whole 16-byte vectors.
@@ -32,7 +31,7 @@ __device__ __forceinline__ void mma_i8(int (&c)[4], unsigned a0, unsigned a1, un
 // in shared memory.  The weights are the multiply's 16 rows and the tokens its 8 columns (NT times).  Which contraction
 // element sits in which place of a fragment does not matter as long as both operands agree, so a lane loads 16 consecutive
 // bytes of its weight rows (g and g + 8) and of its token and uses them as the fragments of two multiplies.
-template <int T, int NT, bool ALIGNED>
+template <int T, int NT, bool ALIGNED, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS)
 linear_rows_kernel(const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue e, uint32_t *status) {
   __shared__ int part[WARPS][16][8 * NT + 1];
@@ -104,12 +103,22 @@ linear_rows_kernel(const int8_t *a, const int8_t *w, int M, int N, int K, const 
 
 int niti_linear_rows(niti_ctx *ctx, cudaStream_t st, const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue &e, int type) {
   const unsigned grid = (unsigned)((N + 15) / 16);
-  auto go = [&](auto tc, auto nt, auto al) -> int {
-    NITI_CUDA_TRY(ctx, niti_launch(st, grid, 32 * WARPS, 0, linear_rows_kernel<decltype(tc)::value, decltype(nt)::value, decltype(al)::value>, a, w, M, N, K,
-                                   e, ctx->d_status));
+  auto go_as = [&](auto tc, auto nt, auto al, auto wc) -> int {
+    constexpr int WARPS = decltype(wc)::value;
+    NITI_CUDA_TRY(ctx, niti_launch(st, grid, 32 * WARPS, 0, linear_rows_kernel<decltype(tc)::value, decltype(nt)::value, decltype(al)::value, WARPS>, a, w,
+                                   M, N, K, e, ctx->d_status));
     ctx->launches++;
     ctx->tc_launches++;
     return NITI_OK;
+  };
+  // Sixteen warps a block where the contraction feeds them and all blocks still run at once (three an SM), else eight: weights
+  // beyond L2, 8 -> 16 warps, 1 x 4096 x 4096 7.5 -> 5.3 us, 32 x 4096 x 4096 13.2 -> 9.9, 1 x 4096 x 16384 25.3 -> 15.4; outside
+  // the rule 1 x 8192 x 4096 9.0 -> 9.2, 16 x 1000 x 512 2.4 -> 2.4.
+  const bool wide = K >= 1024 && (long long)grid <= 3LL * ctx->sm_count;
+  auto go = [&](auto tc, auto nt, auto al) -> int {
+    if constexpr (decltype(al)::value)
+      if (wide) return go_as(tc, nt, al, std::integral_constant<int, 16>{});
+    return go_as(tc, nt, al, std::integral_constant<int, 8>{});
   };
   auto by_rows = [&](auto tc, auto al) -> int {
     if (M <= 8) return go(tc, std::integral_constant<int, 1>{}, al);
