@@ -693,7 +693,7 @@ struct ErrorGrid { int strips, rows, main; };
 // Largest |e| of the tensor, and the column sums of every block's rows; beside them, operands whose rows have to be padded for
 // the multiplies.  Bound: HBM (dout and z are read once here; the rounding pass finds what fits of them in L2).
 template <int T, int VEC, int ACT>
-__global__ void __launch_bounds__(ERR_THREADS)
+__global__ void __launch_bounds__(ERR_THREADS, 8)
 error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int M, int N, ErrorGrid g, PadJob pad0, PadJob pad1,
                  unsigned pad0_blocks) {
   niti_enter(dout, z, pad0.src, pad1.src);
@@ -730,7 +730,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
 // e as payload with the exponent of its maximum, rows of `pitch` bytes.  The rows that the pass before read last come first.
 // Beside it, the bias gradient from that pass' column sums (of `nblk` row blocks).
 template <int T, int VEC, int ACT, bool PSR>
-__global__ void __launch_bounds__(ERR_THREADS)
+__global__ void __launch_bounds__(ERR_THREADS, 8)
 error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, ErrorGrid g,
                    int pitch, const float *part, float *dbias, int nblk) {
   niti_enter(dout, z, hdr, part);
