@@ -31,6 +31,8 @@ __device__ __forceinline__ void mma_i8(int (&c)[4], unsigned a0, unsigned a1, un
 // in shared memory.  The weights are the multiply's 16 rows and the tokens its 8 columns (NT times).  Which contraction
 // element sits in which place of a fragment does not matter as long as both operands agree, so a lane loads 16 consecutive
 // bytes of its weight rows (g and g + 8) and of its token and uses them as the fragments of two multiplies.
+// Weights from HBM: 1 x 8192 x 4096 9.0 us, of which a launch of nothing takes about 1.8 (4.7 TB/s while it streams), 1 x 4096 x
+// 4096 5.6, 32 x 4096 x 4096 9.8 (the tokens come through L2 for every block).  The tiled kernel takes 17.5 us for the first.
 template <int T, int NT, bool ALIGNED, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS)
 linear_rows_kernel(const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue e, uint32_t *status) {
