@@ -496,8 +496,9 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
                         int dw_type, int M, int N, int K, int act, int round_mode, void *ws, size_t ws_bytes);
 
 /* One AdamW step over n tensors (a host array that the call reads before it returns; two of them must not share
- * memory).  0 <= lr, weight_decay <= 1e6, 0 <= beta < 1, 1e-20 <= eps <= 1e6.  With t = *step, the number of this step (device int32, >= 1: a captured graph counts it up between its
- * replays), and g the gradient times *grad_scale (device float32, NULL: 1):
+ * memory).  0 <= lr, weight_decay <= 1e6, 0 <= beta < 1, 1e-20 <= eps <= 1e6.  With t = *step, the number of this step
+ * (device int32, >= 1: a captured graph counts it up between its replays), and g the gradient times *grad_scale (device
+ * float32, NULL: 1):
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps),
  *   w8 <- floor(|p| 2^-s_w + 1/2), at most 127, sign of p (unless w8 is NULL): the int8 weights that the multiplies read,
@@ -512,7 +513,8 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * mix: x ^= x >> 16, x *= 0x7FEB352D, x ^= x >> 15, x *= 0x846CA68B, x ^= x >> 16 in 32 bits.  (To nearest, a state that
  * changes by a thousandth a step would stand still, and one that draws from its own discarded bits does where there is
  * no gradient: the same code times the same constant leaves the same bits.)
- * An element whose scaled gradient is not finite keeps its weight, m and v, and raises NITI_DEV_NONFINITE. */
+ * An element whose scaled gradient is not finite, or 2^63 or more, keeps its weight, m and v, and raises
+ * NITI_DEV_NONFINITE. */
 #define NITI_STATE_BLOCK 256
 typedef struct niti_adamw_tensor {
   float *p;

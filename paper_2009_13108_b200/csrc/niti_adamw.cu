@@ -16,6 +16,7 @@ constexpr int GROUP = 4;                           // chunks that a CTA takes in
 // bytes of a chunk in shared memory: weights, gradients (room for 32 bits), both states
 __host__ __device__ constexpr int stage_bytes(bool eight) { return CHUNK * (4 + 4 + (eight ? 2 : 8)); }
 __host__ __device__ constexpr int ctas_per_sm(bool eight) { return eight ? 4 : 3; }
+constexpr float TOO_LARGE = 9.223372036854775808e18f;   // 2^63: the square of a smaller gradient is finite, and so is every state
 constexpr int LIST_SMALL = 16, LIST_MOST = 256;    // tensors a launch takes (its parameters: 1.4 and 22 KB)
 
 struct Tensor {
@@ -112,7 +113,7 @@ struct Step {                                      // of this step and tensor
 // the integer calls: m mixes a short code and a short gradient with weights 9/10 and 1/10, whose binary expansions repeat the
 // same four bits, and without a gradient a code meets the same constant, and so the same discarded bits, in every step.  A root
 // that is not zero does not round to zero (the next step divides by it).  s_m, s_v: the block's exponents, before and after.
-// Returns whether a gradient was not finite.
+// Returns whether a gradient was not finite, or too large.
 // VEC: the operands are in shared memory at `stage` (the barrier `empty` is told when they have been read), else everything
 // goes by elements.
 template <bool EIGHT, bool VEC>
@@ -191,7 +192,7 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
   float worst = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) worst = niti_absmax(worst, g[j]);
-  const bool bad = !(worst < __int_as_float(0x7f800000));
+  const bool bad = !(worst < TOO_LARGE);
   // The states are products and sums rounded one by one, without fused multiply-adds, and a correctly rounded root: a code
   // follows from them alone, and so from the formulas, whatever computes them.  (By single instructions: the assembler fuses
   // packed multiplications and additions.)
@@ -211,10 +212,10 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
       fma2(rr, F2(st.den_r), F2(st.den_1)).get(d0, d1);
       fma2(mm, F2(reciprocal(d0), reciprocal(d1)), mul2(F2(p[j], p[j + 1]), F2(st.decay))).get(p[j], p[j + 1]);
     }
-  } else {                                         // (elements without a finite gradient keep what they have)
+  } else {                                         // (elements without a usable gradient keep what they have)
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const bool ok = fabsf(g[j]) < __int_as_float(0x7f800000);
+      const bool ok = fabsf(g[j]) < TOO_LARGE;
       if (ok) update(j);
       r[j] = __fsqrt_rn(v[j]);
       if (ok) p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
@@ -307,8 +308,9 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   extern __shared__ __align__(128) char smem[];
   __shared__ __align__(8) unsigned long long bars[2 * STAGES];            // a stage is full, and has been read by all warps
   __shared__ volatile int abort_flag;
-  // exponents of both states for four groups in turn: a warp that begins chunk k + STAGES + 1 waits until all have read chunk
-  // k + 1, and so are done with chunk k
+  // exponents of both states for the groups with chunks that are copied in bulk, in turn: a warp that begins the (k + STAGES +
+  // 1)th of those chunks waits until all have read the (k + 1)th, and so are done with the kth (other chunks make no warp wait,
+  // and so take no turn)
   __shared__ int8_t exps[STAGES + 1][2][GROUP * WARPS];
   __shared__ int arrived[STAGES + 1];
   if (threadIdx.x <= STAGES) arrived[threadIdx.x] = 0;
@@ -370,7 +372,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   // finite and not 0, so that an element without a gradient does not become 0 / 0 or 0 times infinity)
   const float lr = fmaxf(hy.lr / -expm1f((float)t_step * hy.log_b1), 1e-30f);
   st.den_r = -rsqrtf(-expm1f((float)t_step * hy.log_b2)) / lr;
-  st.den_1 = -hy.eps / lr;
+  st.den_1 = -fmaxf(hy.eps / lr, 1e-37f);          // (its reciprocal is finite)
   st.gs = grad_scale ? *grad_scale : 1.0f;
   st.scaled = grad_scale != nullptr;
   st.key = (unsigned)t_step * 0x9E3779B9u;
@@ -382,7 +384,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   int next_m = 0, next_v = 0;                      // exponents of the warp's block of chunk `ready` of tensor `known`
   long long ready = -1;
   bool ok = true;
-  for (int gr = begin, known = -1, turn = 0; ok && gr < end; gr += step_g, turn = turn == STAGES ? 0 : turn + 1) {
+  for (int gr = begin, known = -1, turn = 0; ok && gr < end; gr += step_g) {
     while (gr >= l.first[lo + 1]) ++lo;
     const Tensor &T = l.t[lo];
     if (lo != known) {
@@ -440,6 +442,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
         }
       }
     }
+    if (whole > 0) turn = turn == STAGES ? 0 : turn + 1;
   }
   if (abort_flag) {                                // (as above)
     const long long t0 = clock64();

@@ -106,6 +106,43 @@ def test_many_chunks(niti):
     assert not torch.equal(before, pr["p"][1]) and not whole[:3].any()
 
 
+def test_tensors_that_are_copied_in_bulk_among_others(niti):
+    """A CTA's chunks come from aligned tensors, whose operands are fetched ahead, and from others, in turn: the exponents of
+    one bulk chunk must not meet those of the next where a warp runs ahead over the chunks between them."""
+    sizes = [2048 * 25 + 200 * (i % 3) for i in range(160)]
+    pr = _problem(sizes, 8, torch.bfloat16, True)
+    for i in range(0, len(sizes), 2):
+        buf = torch.zeros(sizes[i] + 1, device="cuda")
+        buf[1:] = pr["p"][i]
+        pr["p"][i] = buf[1:]
+    test_one_step(niti, sizes, torch.bfloat16, 8, True, pr=pr)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_gradients_whose_squares_overflow_leave_their_elements(niti, bits):
+    from paper_2009_13108_b200 import NitiError
+    pr = _problem([4000, 300], bits, torch.float32, True)
+    big = torch.tensor([2.0 ** 63, -3e19, 3e38, 2.0 ** 100], device="cuda")
+    for i, at in ((0, 700), (1, 296)):
+        pr["g"][i][at:at + 4] = big
+        pr["g"][i][at - 1] = 2.0 ** 62
+    was = [(p.clone(), m.clone(), v.clone()) for p, m, v in zip(pr["p"], pr["m"], pr["v"])]
+    niti.adamw(_plan(niti, pr), torch.ones(1, dtype=torch.int32, device="cuda"), LR, (B1, B2), EPS)
+    with pytest.raises(NitiError):
+        niti.check()
+    for i, at in ((0, 700), (1, 296)):
+        assert torch.equal(pr["p"][i][at:at + 4], was[i][0][at:at + 4]) and torch.isfinite(pr["p"][i]).all()
+        # the smaller one is taken: a first step's m / sqrt(v) is about 1 beside its neighbours' states
+        assert not torch.equal(pr["p"][i][at - 1], was[i][0][at - 1])
+        if bits == 32:
+            assert torch.equal(pr["m"][i][at:at + 4], was[i][1][at:at + 4]) and torch.equal(pr["v"][i][at:at + 4], was[i][2][at:at + 4])
+            assert torch.isfinite(pr["v"][i]).all()
+        else:
+            for codes in (pr["m"][i], pr["v"][i]):
+                assert int((codes & 127).max()) <= 126
+            assert int(pr["v"][i].max()) <= 126 and int(pr["s_v"][i].max()) <= 63
+
+
 def test_a_learning_rate_of_zero_changes_the_states_alone(niti):
     for bits in (32, 8):
         pr = _problem([5000], bits, torch.float32, False)
