@@ -644,10 +644,10 @@ class Niti:
         if form is None or size is None or type_id is None:
             raise NitiError(ERR_ARG, "dequantize: int8 or uint8 elements, int32 or int8 exponents, a float result")
         if per is None:
-            per = 0 if count == 1 else q.shape[-1]
+            per = 0 if count == 1 or q.dim() == 0 else q.shape[-1]
         if n and count != (-(-n // per) if per > 0 else 1 if block is None else -1):
             raise NitiError(ERR_ARG, "dequantize: %d exponents for %d elements, %s each" % (count, n, per or "all"))
-        if out is None and q.dim() <= 2:
+        if out is None and 1 <= q.dim() <= 2:
             out = self._new(q.shape, dtype)
         elif out is None:
             out = torch.empty(q.shape, dtype=dtype, device=self.device)

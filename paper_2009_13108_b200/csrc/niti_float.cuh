@@ -183,7 +183,9 @@ __device__ __forceinline__ unsigned niti_unit_mag(float x, float scale) {
     const unsigned v = __float_as_uint(__fadd_rz(fminf(fabsf(x) * scale, 127.0f * 65536.0f), 8388608.0f));
     return v + (~v & 255u) * 256u;
   } else {
-    return __float_as_uint(__fadd_rz(fminf(fmaf(fabsf(x), scale, 0.5f), 127.0f), 8388608.0f));
+    // (plus the float below 1/2, 1/2 - 2^-25: 1/2 itself would lift a magnitude of 1/2 - 2^-25 to 1 by the sum's rounding, and
+    // what is missing from k + 1/2 to k + 1 the rounding adds, half a step below 1 and less below the others)
+    return __float_as_uint(__fadd_rz(fminf(fmaf(fabsf(x), scale, 0.49999997f), 127.0f), 8388608.0f));
   }
 }
 // (of 127 << 16 the sum is 127 << 16 | 0xff00: the same byte)

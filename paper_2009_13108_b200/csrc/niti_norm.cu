@@ -52,6 +52,10 @@ __device__ __forceinline__ unsigned row_top(unsigned am, float ss, float r) {
   return am >= INF_BITS || !(ss < __uint_as_float(INF_BITS)) ? INF_BITS : __float_as_uint(__uint_as_float(am) * r);
 }
 
+// r and the factor from payload units usually scale a value in one product.  Where r is large (rows near zero with a tiny eps)
+// that factor can leave float32: r is applied first then.  2^11 2^100 2^16 is 2^127.
+constexpr float LARGE_R = 2048.0f;
+
 // y = h r gain with h = x + residual, r = 1 / sqrt(mean(h^2) + eps); without NORM y = x.  A thread holds NV vectors of its
 // row, and the next row's are on their way while this one's sums are taken.  The maximum that fixes the exponent is taken
 // of |h gain| beside the sum of squares, since r only scales it: one reduction a row.
@@ -130,7 +134,14 @@ norm_rows_kernel(const void *x, const void *res, const float *gain, void *h, int
       continue;
     }
     const int s = niti_exponent_of(top);
-    const float scale = niti_payload_scale(r * niti_pow2(-s), round_mode);
+    const bool large = NORM && r > LARGE_R;
+    if (large) {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) hv[v][j] *= r;
+    }
+    const float scale = niti_payload_scale((large ? 1.0f : r) * niti_pow2(-s), round_mode);
     if (t == 0 && rok) s_y[row] = s;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -157,12 +168,18 @@ norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y
     const int row = M - 1 - (int)(it / parts), part = (int)(it % parts);
     const int c = (part * ROW_THREADS + (int)threadIdx.x) * VEC;
     if (c >= C) continue;
-    const float scale = niti_payload_scale(NORM ? rstd[row] * p2 : p2, round_mode);
+    const float r = NORM ? rstd[row] : 1.0f;
+    const bool large = NORM && r > LARGE_R;
+    const float scale = niti_payload_scale((large ? 1.0f : r) * p2, round_mode);
     Pack<T, VEC> p;
     p.load(h, (long long)row * C + c);
     float v[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; ++j) v[j] = NORM ? p.get(j) * gain[c + j] : p.get(j);
+    if (large) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] *= r;
+    }
     store_payload<VEC, MODE>(y, (long long)row * C + c, v, scale, round_mode);
   }
 }
@@ -207,13 +224,14 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
       continue;
     }
     const int s = niti_exponent_of(top);
-    const float scale = niti_payload_scale(r * niti_pow2(-s), round_mode);
+    const bool large = NORM && r > LARGE_R;
+    const float scale = niti_payload_scale((large ? 1.0f : r) * niti_pow2(-s), round_mode);
     if (threadIdx.x == 0) s_y[row] = s;
     const void *src = NORM && res ? h : x;            // (each thread reads what it has written itself)
     for (int c = (int)threadIdx.x; c < C; c += 1024) {
       Pack<T, 1> p;
       p.load(src, at + c);
-      const float v[1] = {NORM ? p.get(0) * gain[c] : p.get(0)};
+      const float v[1] = {NORM ? p.get(0) * gain[c] * (large ? r : 1.0f) : p.get(0)};
       store_payload<1, ROUND_BY_ARGUMENT>(y, at + c, v, scale, round_mode);
     }
   }
@@ -224,15 +242,19 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
 // columns of a thread are the same in every row, so the gain's gradient stays in its registers; each block leaves its sums
 // in `part` and column_sum_kernel adds them up in a fixed order.  8192 x 4096 bfloat16 with dh: 268 MB in 42 us, 6.4 TB/s (0.99
 // of the measured copy rate), and 5 us for the sums of 296 blocks.
-template <int T, int VEC, int NV>
-__global__ void __launch_bounds__(ROW_MOST)
+// (The register limit is stated because the compiler, left to choose, compiled the widest instance for 32 registers: 4096 x 8192
+// took 513 us, now 57 with the sums.)
+// AHEAD: the next row's operands are on their way in registers of their own.  Thirty-two columns a thread leave no room for
+// that (nor for the gain, which then comes from L1).
+template <int T, int VEC, int NV, bool AHEAD = NV * VEC < 32>
+__global__ void __launch_bounds__(ROW_MOST, 1)
 norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, float *part,
                 RowShape sh) {
   __shared__ float2 buf[2][32];
   niti_enter(dy, h, gain, rstd, dh);
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const int grp = (int)threadIdx.x / sh.tpr, t = (int)threadIdx.x - grp * sh.tpr;
-  float g[NV][VEC], dg[NV][VEC];
+  float g[AHEAD ? NV : 1][VEC], dg[NV][VEC];
   Pack<T, VEC> py[NV], ph[NV], pd[NV];
   bool in[NV];
 #pragma unroll
@@ -242,10 +264,15 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
     py[v].zero(); ph[v].zero(); pd[v].zero();
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      g[v][j] = in[v] ? gain[c + j] : 0.0f;
+      if (AHEAD) g[v][j] = in[v] ? gain[c + j] : 0.0f;
       dg[v][j] = 0.0f;
     }
   }
+  auto gain_of = [&](int v, float (&k)[VEC]) {
+    const int c = (v * sh.tpr + t) * VEC;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) k[j] = AHEAD ? g[AHEAD ? v : 0][j] : in[v] ? __ldg(gain + c + j) : 0.0f;
+  };
   const int step = (int)gridDim.x * sh.rpb;
   float r_next = 0.0f;
   auto fetch = [&](int row) {
@@ -261,36 +288,53 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
       }
   };
   int row = (int)blockIdx.x * sh.rpb + grp;
-  fetch(row);
+  if (AHEAD) fetch(row);
   for (int turn = 0, base = (int)blockIdx.x * sh.rpb; base < sh.M; base += step, row += step, turn ^= 1) {
     const bool rok = row < sh.M;
+    if (!AHEAD) fetch(row);
     const float r = r_next;
-    Pack<T, VEC> qy[NV], qh[NV], qd[NV];
     float dot = 0.0f;
+    // (sums of a row, then its result: from copies where the next row's operands take the places of this one's)
+    auto sums = [&](const Pack<T, VEC> (&qy)[NV], const Pack<T, VEC> (&qh)[NV]) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      qy[v] = py[v]; qh[v] = ph[v]; qd[v] = pd[v];
-    }
-    fetch(row + step);
+      for (int v = 0; v < NV; ++v) {
+        float k[VEC];
+        gain_of(v, k);
 #pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float y = qy[v].get(j), hh = qh[v].get(j);
-        dot = fmaf(y * g[v][j], hh, dot);
-        if (rok) dg[v][j] = fmaf(y, hh * r, dg[v][j]);
+        for (int j = 0; j < VEC; ++j) {
+          const float y = qy[v].get(j), hh = qh[v].get(j);
+          dot = fmaf(y * k[j], hh, dot);
+          if (rok) dg[v][j] = fmaf(y, hh * r, dg[v][j]);
+        }
       }
-    unsigned none = 0;
-    row_reduce(dot, none, sh.tpr, warp, lane, buf, turn);
-    const float c = dot / (float)sh.C * (r * r * r);
+    };
+    auto result = [&](const Pack<T, VEC> (&qy)[NV], const Pack<T, VEC> (&qh)[NV], const Pack<T, VEC> (&qd)[NV]) {
+      unsigned none = 0;
+      row_reduce(dot, none, sh.tpr, warp, lane, buf, turn);
+      const float c = dot / (float)sh.C * r * r * r; // (r^3 alone can leave float32)
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      float d[VEC];
+      for (int v = 0; v < NV; ++v) {
+        float k[VEC], d[VEC];
+        gain_of(v, k);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) d[j] = qd[v].get(j) + (r * (qy[v].get(j) * g[v][j]) - c * qh[v].get(j));
-      Pack<T, VEC> o;
-      o.set(d);
-      if (in[v] && rok) o.store(dx, (long long)row * sh.C + (v * sh.tpr + t) * VEC);
+        for (int j = 0; j < VEC; ++j) d[j] = qd[v].get(j) + (r * (qy[v].get(j) * k[j]) - c * qh[v].get(j));
+        Pack<T, VEC> o;
+        o.set(d);
+        if (in[v] && rok) o.store(dx, (long long)row * sh.C + (v * sh.tpr + t) * VEC);
+      }
+    };
+    if constexpr (AHEAD) {
+      Pack<T, VEC> qy[NV], qh[NV], qd[NV];
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        qy[v] = py[v]; qh[v] = ph[v]; qd[v] = pd[v];
+      }
+      fetch(row + step);
+      sums(qy, qh);
+      result(qy, qh, qd);
+    } else {
+      sums(py, ph);
+      result(py, ph, pd);
     }
   }
   if (!part) return;
@@ -332,7 +376,7 @@ norm_bwd_wide_kernel(const void *dy, const void *h, const float *gain, const flo
       dot = fmaf(a.get(0) * gain[c], b.get(0), dot);
     }
     row_reduce(dot, none, 1024, warp, lane, buf, turn);
-    const float k = dot / (float)C * (r * r * r);
+    const float k = dot / (float)C * r * r * r;
     for (int c = (int)threadIdx.x; c < C; c += 1024) {
       a.load(dy, at + c);
       b.load(h, at + c);
@@ -370,8 +414,9 @@ column_sum_kernel(const float *part, float *dst, int n, int C) {
   niti_column_sums<W, 32>(part, dst, n, C, (int)blockIdx.x, buf);
 }
 
+// 2^e, e clamped to the format's -128 .. 127
 __device__ __forceinline__ float exponent_scale(int e) {
-  return e >= -126 && e <= 127 ? niti_pow2(e) : ldexpf(1.0f, e < -149 ? -149 : e > 128 ? 128 : e);
+  return e >= 127 ? niti_pow2(127) : e >= -126 ? niti_pow2(e) : __int_as_float(e == -127 ? 0x00400000 : 0x00200000);
 }
 // (an e4m3 code's exponent and fraction, moved into place, are the value over 2^120; exact, the small ones too)
 template <bool E4M3>
@@ -605,7 +650,9 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
     return niti_fail(ctx, NITI_ERR_ARG, "niti_rmsnorm_bwd: bad argument (pointers are aligned to their type)");
   float *part = dgain ? (float *)((char *)ws + NITI_WS_HEADER) : nullptr;
   const bool aligned = (((uintptr_t)dy | (uintptr_t)h | (uintptr_t)dh | (uintptr_t)dx) & 15) == 0;
-  const RowPlan pl = plan_rows(M, C, type, aligned, 4);
+  // (512 threads with two vectors before 256 with four, whose operands fill the registers)
+  RowPlan pl = plan_rows(M, C, type, aligned, 2);
+  if (!pl.nv) pl = plan_rows(M, C, type, aligned, 4);
   int nparts = 0;
   rc = with_type(type, [&](auto t) -> int {
     constexpr int T = decltype(t)::value;

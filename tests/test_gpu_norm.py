@@ -125,6 +125,61 @@ def test_extreme_magnitudes_keep_the_exponents_bounds(niti, value):
     assert niti.check() == 0
 
 
+def test_rounding_to_nearest_is_exact_beside_halves(niti):
+    """Magnitudes k + 1/2 and the floats around them, in units: 2^-25 below 1/2 is 0, and every half goes up."""
+    half = np.arange(0, 127, dtype=np.float32) + np.float32(0.5)
+    u = np.concatenate([half, np.nextafter(half, np.float32(0)), np.nextafter(half, np.float32(200))])
+    u = np.concatenate([u, -u, [np.float32(127)]]).astype(np.float32)
+    want = np.sign(u) * np.minimum(np.floor(np.abs(u.astype(np.float64)) + 0.5), 127)
+    for pad in (0, 2):                                    # (rows of whole vectors, and of single elements)
+        x = torch.from_numpy(np.pad(u, (0, -u.size % 4 + pad))).cuda().view(1, -1)
+        q, s = niti.quantize(x)
+        assert int(s) == 0 and np.array_equal(_np(q)[0, :u.size], want)
+
+
+@pytest.mark.parametrize("C", [33, 256, 16400])
+@pytest.mark.parametrize("rows", [True, False])
+@pytest.mark.parametrize("mode", [0, 1])
+@pytest.mark.parametrize("power", [-123, -118, -90])
+def test_rows_near_zero_with_a_tiny_eps(niti, C, rows, mode, power):
+    """1 / rms is 1e6 here, and together with 2^100 and the 16 fraction bits it is no float32."""
+    x = _rows(31, 5, C, torch.float32) * 2.0 ** power
+    x[:, ::3] = 0
+    x[3] = 0
+    gain = 1 + 0.3 * torch.randn(C, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    y, s, _, rstd = niti.rmsnorm_fwd(x, gain, rows=rows, eps=1e-12, round_mode=mode)
+    v = _np(x) * _np(gain) / np.sqrt((_np(x) ** 2).mean(1, keepdims=True) + float(np.float32(1e-12)))
+    top = np.abs(v).max(1, keepdims=True) if rows else np.abs(v).max().reshape(1, 1)
+    assert np.array_equal(s.cpu().numpy().reshape(-1, 1), exponents(top))
+    # (products below 2^-126 lose bits: up to 2^-150 of h gain, times 1e6 and 2^100, in units)
+    check_payload(y.cpu().numpy(), s.cpu().numpy().reshape(-1, 1), v, mode, _slack(C) + 2.0 ** -149 * 1e6 * 2.0 ** 100)
+    assert not y[:, ::3].any() and not y[3].any() and niti.check() == 0
+
+
+@pytest.mark.parametrize("C", [256, 16400])
+def test_backward_of_rows_near_zero(niti, C):
+    """r is 2^50: its cube is no float32, what it is multiplied with makes the product one."""
+    h, dy = _rows(32, 3, C, torch.float32) * 2.0 ** -50, _rows(33, 3, C, torch.float32) * 2.0 ** -50
+    rstd = torch.rsqrt(h.double().square().mean(1)).float()
+    dx, _ = niti.rmsnorm_bwd(dy, h, torch.ones(C, device="cuda"), rstd)
+    H, Y, r = _np(h), _np(dy), _np(rstd)[:, None]
+    want = r * Y - H * r ** 3 * (Y * H).mean(1, keepdims=True)
+    terms = np.abs(r * Y) + np.abs(H) * r ** 3 * np.abs(Y * H).mean(1, keepdims=True)
+    assert np.all(np.abs(_np(dx) - want) <= terms * (max(32, C / 512) + 20) * 2.0 ** -24)
+
+
+def test_dequantize_at_the_ends_of_the_exponents(niti):
+    q = torch.tensor([[0, 1, 127, -127] * 8] * 6, dtype=torch.int8, device="cuda")
+    s = torch.tensor([127, 200, -126, -127, -128, -200], dtype=torch.int32, device="cuda")
+    for shape in (q, q[:, :4].contiguous()):
+        v = _np(niti.dequantize(shape, s))
+        want = _np(shape) * np.exp2(np.clip(s.cpu().numpy().astype(float), -128, 127))[:, None]
+        want[np.abs(want) >= 2.0 ** 128] = np.inf * np.sign(want[np.abs(want) >= 2.0 ** 128])
+        assert np.array_equal(v, want)
+    one = niti.dequantize(torch.tensor(5, dtype=torch.int8, device="cuda"), s[2:3])
+    assert one.shape == () and float(one) == 5 * 2.0 ** -126
+
+
 def test_calls_without_rows_do_nothing(niti):
     gain = torch.ones(64, device="cuda")
     y, s, h, rstd = niti.rmsnorm_fwd(torch.empty((0, 64), device="cuda"), gain)
