@@ -184,8 +184,9 @@ norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y
   }
 }
 
-// Rows that are longer than a block's registers: the row is read again (from L2) for the rounding.
-template <int T, bool NORM, bool SHARED>
+// Rows that are longer than a block's registers: the row is read again (from L2) for the rounding.  2048 x 16384
+// float32 with a residual 109 us, 4.0 TB/s; by single elements 123.
+template <int T, int VEC, bool NORM, bool SHARED>
 __global__ void __launch_bounds__(1024)
 norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int8_t *y, int32_t *s_y, float *rstd,
                  WsHeader *hdr, WsHeader *next, uint32_t *status, int M, int C, float eps, int round_mode) {
@@ -198,18 +199,22 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
   for (int row = (int)blockIdx.x; row < M; row += (int)gridDim.x, turn ^= 1) {
     const long long at = (long long)row * C;
     float ss = 0.0f, am = 0.0f;
-    for (int c = (int)threadIdx.x; c < C; c += 1024) {
-      Pack<T, 1> p;
-      p.load(x, at + c);
+#pragma unroll 4
+    for (int c = (int)threadIdx.x * VEC; c < C; c += 1024 * VEC) {
+      Pack<T, VEC> p;
+      p.template load<true>(x, at + c);
       if (NORM && res) {
-        Pack<T, 1> pr;
+        Pack<T, VEC> pr;
         pr.load(res, at + c);
         p.add(pr);
         p.store(h, at + c);
       }
-      const float v = p.get(0);
-      if (NORM) ss = fmaf(v, v, ss);
-      am = niti_absmax(am, NORM ? v * gain[c] : v);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float v = p.get(j);
+        if (NORM) ss = fmaf(v, v, ss);
+        am = niti_absmax(am, NORM ? v * gain[c + j] : v);
+      }
     }
     unsigned ab = __float_as_uint(am);
     row_reduce(ss, ab, 1024, warp, lane, buf, turn);
@@ -228,11 +233,14 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
     const float scale = niti_payload_scale((large ? 1.0f : r) * niti_pow2(-s), round_mode);
     if (threadIdx.x == 0) s_y[row] = s;
     const void *src = NORM && res ? h : x;            // (each thread reads what it has written itself)
-    for (int c = (int)threadIdx.x; c < C; c += 1024) {
-      Pack<T, 1> p;
+#pragma unroll 2
+    for (int c = (int)threadIdx.x * VEC; c < C; c += 1024 * VEC) {
+      Pack<T, VEC> p;
       p.load(src, at + c);
-      const float v[1] = {NORM ? p.get(0) * gain[c] * (large ? r : 1.0f) : p.get(0)};
-      store_payload<1, ROUND_BY_ARGUMENT>(y, at + c, v, scale, round_mode);
+      float v[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] = NORM ? p.get(j) * gain[c + j] * (large ? r : 1.0f) : p.get(j);
+      store_payload<VEC, ROUND_BY_ARGUMENT>(y, at + c, v, scale, round_mode);
     }
   }
   if (SHARED && threadIdx.x == 0 && most) atomicMax(&hdr->maxabs32, most);
@@ -242,11 +250,9 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
 // columns of a thread are the same in every row, so the gain's gradient stays in its registers; each block leaves its sums
 // in `part` and column_sum_kernel adds them up in a fixed order.  8192 x 4096 bfloat16 with dh: 268 MB in 42 us, 6.4 TB/s (0.99
 // of the measured copy rate), and 5 us for the sums of 296 blocks.
-// (The register limit is stated because the compiler, left to choose, compiled the widest instance for 32 registers: 4096 x 8192
-// took 513 us, now 57 with the sums.)
-// AHEAD: the next row's operands are on their way in registers of their own.  Thirty-two columns a thread leave no room for
-// that (nor for the gain, which then comes from L1).
-template <int T, int VEC, int NV, bool AHEAD = NV * VEC < 32>
+// At most 16 columns of a thread in 16 bits: with 32 their operands, gains and sums do not fit 128 registers (4096 x 8192 bfloat16
+// as 256 threads of 32 columns took 513 us in spilled registers, as 512 of 16 it takes 57).
+template <int T, int VEC, int NV>
 __global__ void __launch_bounds__(ROW_MOST, 1)
 norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, float *part,
                 RowShape sh) {
@@ -254,7 +260,7 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
   niti_enter(dy, h, gain, rstd, dh);
   const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
   const int grp = (int)threadIdx.x / sh.tpr, t = (int)threadIdx.x - grp * sh.tpr;
-  float g[AHEAD ? NV : 1][VEC], dg[NV][VEC];
+  float g[NV][VEC], dg[NV][VEC];
   Pack<T, VEC> py[NV], ph[NV], pd[NV];
   bool in[NV];
 #pragma unroll
@@ -264,15 +270,10 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
     py[v].zero(); ph[v].zero(); pd[v].zero();
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      if (AHEAD) g[v][j] = in[v] ? gain[c + j] : 0.0f;
+      g[v][j] = in[v] ? gain[c + j] : 0.0f;
       dg[v][j] = 0.0f;
     }
   }
-  auto gain_of = [&](int v, float (&k)[VEC]) {
-    const int c = (v * sh.tpr + t) * VEC;
-#pragma unroll
-    for (int j = 0; j < VEC; ++j) k[j] = AHEAD ? g[AHEAD ? v : 0][j] : in[v] ? __ldg(gain + c + j) : 0.0f;
-  };
   const int step = (int)gridDim.x * sh.rpb;
   float r_next = 0.0f;
   auto fetch = [&](int row) {
@@ -288,53 +289,36 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
       }
   };
   int row = (int)blockIdx.x * sh.rpb + grp;
-  if (AHEAD) fetch(row);
+  fetch(row);
   for (int turn = 0, base = (int)blockIdx.x * sh.rpb; base < sh.M; base += step, row += step, turn ^= 1) {
     const bool rok = row < sh.M;
-    if (!AHEAD) fetch(row);
     const float r = r_next;
+    Pack<T, VEC> qy[NV], qh[NV], qd[NV];
     float dot = 0.0f;
-    // (sums of a row, then its result: from copies where the next row's operands take the places of this one's)
-    auto sums = [&](const Pack<T, VEC> (&qy)[NV], const Pack<T, VEC> (&qh)[NV]) {
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float k[VEC];
-        gain_of(v, k);
+    for (int v = 0; v < NV; ++v) {
+      qy[v] = py[v]; qh[v] = ph[v]; qd[v] = pd[v];
+    }
+    fetch(row + step);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-          const float y = qy[v].get(j), hh = qh[v].get(j);
-          dot = fmaf(y * k[j], hh, dot);
-          if (rok) dg[v][j] = fmaf(y, hh * r, dg[v][j]);
-        }
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const float y = qy[v].get(j), hh = qh[v].get(j);
+        dot = fmaf(y * g[v][j], hh, dot);
+        if (rok) dg[v][j] = fmaf(y, hh * r, dg[v][j]);
       }
-    };
-    auto result = [&](const Pack<T, VEC> (&qy)[NV], const Pack<T, VEC> (&qh)[NV], const Pack<T, VEC> (&qd)[NV]) {
-      unsigned none = 0;
-      row_reduce(dot, none, sh.tpr, warp, lane, buf, turn);
-      const float c = dot / (float)sh.C * r * r * r; // (r^3 alone can leave float32)
+    unsigned none = 0;
+    row_reduce(dot, none, sh.tpr, warp, lane, buf, turn);
+    const float c = dot / (float)sh.C * r * r * r;   // (r^3 alone can leave float32)
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        float k[VEC], d[VEC];
-        gain_of(v, k);
+    for (int v = 0; v < NV; ++v) {
+      float d[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) d[j] = qd[v].get(j) + (r * (qy[v].get(j) * k[j]) - c * qh[v].get(j));
-        Pack<T, VEC> o;
-        o.set(d);
-        if (in[v] && rok) o.store(dx, (long long)row * sh.C + (v * sh.tpr + t) * VEC);
-      }
-    };
-    if constexpr (AHEAD) {
-      Pack<T, VEC> qy[NV], qh[NV], qd[NV];
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        qy[v] = py[v]; qh[v] = ph[v]; qd[v] = pd[v];
-      }
-      fetch(row + step);
-      sums(qy, qh);
-      result(qy, qh, qd);
-    } else {
-      sums(py, ph);
-      result(py, ph, pd);
+      for (int j = 0; j < VEC; ++j) d[j] = qd[v].get(j) + (r * (qy[v].get(j) * g[v][j]) - c * qh[v].get(j));
+      Pack<T, VEC> o;
+      o.set(d);
+      if (in[v] && rok) o.store(dx, (long long)row * sh.C + (v * sh.tpr + t) * VEC);
     }
   }
   if (!part) return;
@@ -354,9 +338,9 @@ norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *r
   }
 }
 
-// Backward of rows longer than a block's registers: one block per row reads it twice and leaves dy h r to be summed by
-// columns in a second pass (norm_wide_gain_kernel).
-template <int T>
+// Backward of rows longer than a block's registers: one block per row reads it twice (the second time from L2) and leaves dy h r
+// to be summed by columns in another pass (norm_wide_gain_kernel).  2048 x 16384 float32 144 us, single elements 222.
+template <int T, int VEC>
 __global__ void __launch_bounds__(1024)
 norm_bwd_wide_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, int M, int C) {
   __shared__ float2 buf[2][32];
@@ -368,42 +352,53 @@ norm_bwd_wide_kernel(const void *dy, const void *h, const float *gain, const flo
     const float r = rstd[row];
     float dot = 0.0f;
     unsigned none = 0;
-    Pack<T, 1> a, b, d;
+    Pack<T, VEC> a, b, d;
     d.zero();
-    for (int c = (int)threadIdx.x; c < C; c += 1024) {
-      a.load(dy, at + c);
-      b.load(h, at + c);
-      dot = fmaf(a.get(0) * gain[c], b.get(0), dot);
+#pragma unroll 4
+    for (int c = (int)threadIdx.x * VEC; c < C; c += 1024 * VEC) {
+      a.template load<true>(dy, at + c);
+      b.template load<true>(h, at + c);
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) dot = fmaf(a.get(j) * gain[c + j], b.get(j), dot);
     }
     row_reduce(dot, none, 1024, warp, lane, buf, turn);
     const float k = dot / (float)C * r * r * r;
-    for (int c = (int)threadIdx.x; c < C; c += 1024) {
+#pragma unroll 2
+    for (int c = (int)threadIdx.x * VEC; c < C; c += 1024 * VEC) {
       a.load(dy, at + c);
       b.load(h, at + c);
       if (dh) d.load(dh, at + c);
-      const float o[1] = {d.get(0) + (r * (a.get(0) * gain[c]) - k * b.get(0))};
-      Pack<T, 1> po;
+      float o[VEC];
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) o[j] = d.get(j) + (r * (a.get(j) * gain[c + j]) - k * b.get(j));
+      Pack<T, VEC> po;
       po.set(o);
       po.store(dx, at + c);
     }
   }
 }
-// Column sums of dy h r over a share of the rows (blockIdx.y), a thread per column; in front of norm_bwd_wide_kernel, which
+// Column sums of dy h r over a share of the rows (blockIdx.y), VEC columns a thread; in front of norm_bwd_wide_kernel, which
 // may write dx over dy.
-template <int T>
+template <int T, int VEC>
 __global__ void __launch_bounds__(256)
 norm_wide_gain_kernel(const void *dy, const void *h, const float *rstd, float *part, int M, int C) {
   niti_enter(dy, h, rstd);
-  const int c = (int)(blockIdx.x * 256 + threadIdx.x);
+  const int c = (int)(blockIdx.x * 256 + threadIdx.x) * VEC;
   if (c >= C) return;
-  float sum = 0.0f;
+  float sum[VEC];
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) sum[j] = 0.0f;
+#pragma unroll 4
   for (int row = (int)blockIdx.y; row < M; row += (int)gridDim.y) {
-    Pack<T, 1> a, b;
+    Pack<T, VEC> a, b;
     a.load(dy, (long long)row * C + c);
     b.load(h, (long long)row * C + c);
-    sum = fmaf(a.get(0), b.get(0) * rstd[row], sum);
+    const float r = rstd[row];
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) sum[j] = fmaf(a.get(j), b.get(j) * r, sum[j]);
   }
-  part[(long long)blockIdx.y * C + c] = sum;
+#pragma unroll
+  for (int j = 0; j < VEC; ++j) part[(long long)blockIdx.y * C + c + j] = sum[j];
 }
 
 template <int W>
@@ -550,10 +545,13 @@ int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
         return rows(vec, std::integral_constant<int, 4>{});
       };
       if (!pl.nv) {
-        NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(c.M < 2 * ctx->sm_count ? c.M : 2 * ctx->sm_count), 1024, 0,
-                                       norm_wide_kernel<T, NORM, SHARED>, c.x, c.res, c.gain, c.h, c.y, c.s_y, rstd, hdr, next, ctx->d_status,
-                                       c.M, c.C, c.eps, c.round_mode));
-        return NITI_OK;
+        auto wide = [&](auto vec) -> int {
+          NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(c.M < 2 * ctx->sm_count ? c.M : 2 * ctx->sm_count), 1024, 0,
+                                         norm_wide_kernel<T, decltype(vec)::value, NORM, SHARED>, c.x, c.res, c.gain, c.h, c.y, c.s_y, rstd, hdr, next,
+                                         ctx->d_status, c.M, c.C, c.eps, c.round_mode));
+          return NITI_OK;
+        };
+        return pl.vec == 1 ? wide(std::integral_constant<int, 1>{}) : wide(std::integral_constant<int, V16>{});
       }
       return pl.vec == 1 ? pick(std::integral_constant<int, 1>{}) : pick(std::integral_constant<int, V16>{});
     };
@@ -650,23 +648,28 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
     return niti_fail(ctx, NITI_ERR_ARG, "niti_rmsnorm_bwd: bad argument (pointers are aligned to their type)");
   float *part = dgain ? (float *)((char *)ws + NITI_WS_HEADER) : nullptr;
   const bool aligned = (((uintptr_t)dy | (uintptr_t)h | (uintptr_t)dh | (uintptr_t)dx) & 15) == 0;
-  // (512 threads with two vectors before 256 with four, whose operands fill the registers)
+  // (512 threads with two vectors before 256 with four)
   RowPlan pl = plan_rows(M, C, type, aligned, 2);
-  if (!pl.nv) pl = plan_rows(M, C, type, aligned, 4);
+  if (!pl.nv && pl.vec < 8) pl = plan_rows(M, C, type, aligned, 4);
   int nparts = 0;
   rc = with_type(type, [&](auto t) -> int {
     constexpr int T = decltype(t)::value;
     constexpr int V16 = 16 / (int)sizeof(typename FloatOf<T>::type);
     if (!pl.nv) {
-      if (dgain) {
-        nparts = M < BWD_PARTS ? M : BWD_PARTS;
-        NITI_CUDA_TRY(ctx, niti_launch(st, dim3((unsigned)((C + 255) / 256), (unsigned)nparts), 256, 0, norm_wide_gain_kernel<T>, dy, h, rstd,
-                                       part, M, C));
-        ctx->launches++;
-      }
-      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(M < 2 * ctx->sm_count ? M : 2 * ctx->sm_count), 1024, 0, norm_bwd_wide_kernel<T>, dy, h, gain,
-                                     rstd, dh, dx, M, C));
-      return NITI_OK;
+      auto wide = [&](auto vec) -> int {
+        constexpr int VEC = decltype(vec)::value;
+        if (dgain) {
+          const int strips = (C + 256 * VEC - 1) / (256 * VEC), most = 8 * ctx->sm_count / strips;     // (one wave)
+          nparts = most < 1 ? 1 : most < BWD_PARTS ? most : BWD_PARTS;
+          if (nparts > M) nparts = M;
+          NITI_CUDA_TRY(ctx, niti_launch(st, dim3((unsigned)strips, (unsigned)nparts), 256, 0, norm_wide_gain_kernel<T, VEC>, dy, h, rstd, part, M, C));
+          ctx->launches++;
+        }
+        NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(M < 2 * ctx->sm_count ? M : 2 * ctx->sm_count), 1024, 0, norm_bwd_wide_kernel<T, VEC>, dy, h, gain,
+                                       rstd, dh, dx, M, C));
+        return NITI_OK;
+      };
+      return pl.vec == 1 ? wide(std::integral_constant<int, 1>{}) : wide(std::integral_constant<int, V16>{});
     }
     const int threads = pl.sh.tpr * pl.sh.rpb;
     unsigned blocks = row_blocks(ctx, pl.sh, threads, 512);
@@ -680,8 +683,10 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
     };
     auto pick = [&](auto vec) -> int {
       if (pl.nv == 1) return rows(vec, std::integral_constant<int, 1>{});
-      if (pl.nv == 2) return rows(vec, std::integral_constant<int, 2>{});
-      return rows(vec, std::integral_constant<int, 4>{});
+      constexpr int VEC = decltype(vec)::value;
+      if constexpr (VEC < 8)
+        if (pl.nv == 4) return rows(vec, std::integral_constant<int, 4>{});
+      return rows(vec, std::integral_constant<int, 2>{});
     };
     return pl.vec == 1 ? pick(std::integral_constant<int, 1>{}) : pick(std::integral_constant<int, V16>{});
   });
