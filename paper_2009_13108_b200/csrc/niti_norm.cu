@@ -513,7 +513,9 @@ template <bool NORM>
 int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
   const uintptr_t all = (uintptr_t)c.x | (uintptr_t)c.res | (uintptr_t)c.h;
   const bool aligned = (all & 15) == 0 && !misaligned(c.y, 8);
-  const RowPlan pl = plan_rows(c.M, c.C, c.type, aligned, 4);
+  // (at most 16 columns a thread before 32: 8192 x 5120 bfloat16 66 -> 55 us; float32 as 512 threads of 8, 8192 x 4096 shared 73 -> 89)
+  RowPlan pl = plan_rows(c.M, c.C, c.type, aligned, c.type == NITI_F32 ? 4 : 2);
+  if (!pl.nv) pl = plan_rows(c.M, c.C, c.type, aligned, 4);
   WsHeader *hdr = nullptr, *next = nullptr;
   float *rstd = c.rstd;
   if (!c.rows) {
