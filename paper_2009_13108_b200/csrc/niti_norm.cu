@@ -513,9 +513,10 @@ template <bool NORM>
 int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
   const uintptr_t all = (uintptr_t)c.x | (uintptr_t)c.res | (uintptr_t)c.h;
   const bool aligned = (all & 15) == 0 && !misaligned(c.y, 8);
-  // (at most 16 columns a thread before 32: 8192 x 5120 bfloat16 66 -> 55 us; float32 as 512 threads of 8, 8192 x 4096 shared 73 -> 89)
+  // (at most 16 columns a thread before 32: 8192 x 5120 bfloat16 66 -> 55 us; float32 as 512 threads of 8, 8192 x 4096 shared 73
+  // -> 89.  Single elements: up to 16 a thread)
   RowPlan pl = plan_rows(c.M, c.C, c.type, aligned, c.type == NITI_F32 ? 4 : 2);
-  if (!pl.nv) pl = plan_rows(c.M, c.C, c.type, aligned, 4);
+  if (!pl.nv) pl = plan_rows(c.M, c.C, c.type, aligned, pl.vec == 1 ? 16 : 4);
   WsHeader *hdr = nullptr, *next = nullptr;
   float *rstd = c.rstd;
   if (!c.rows) {
@@ -544,6 +545,10 @@ int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
       auto pick = [&](auto vec) -> int {
         if (pl.nv == 1) return rows(vec, std::integral_constant<int, 1>{});
         if (pl.nv == 2) return rows(vec, std::integral_constant<int, 2>{});
+        if constexpr (decltype(vec)::value == 1) {
+          if (pl.nv == 8) return rows(vec, std::integral_constant<int, 8>{});
+          if (pl.nv == 16) return rows(vec, std::integral_constant<int, 16>{});
+        }
         return rows(vec, std::integral_constant<int, 4>{});
       };
       if (!pl.nv) {
@@ -652,7 +657,7 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
   const bool aligned = (((uintptr_t)dy | (uintptr_t)h | (uintptr_t)dh | (uintptr_t)dx) & 15) == 0;
   // (512 threads with two vectors before 256 with four)
   RowPlan pl = plan_rows(M, C, type, aligned, 2);
-  if (!pl.nv && pl.vec < 8) pl = plan_rows(M, C, type, aligned, 4);
+  if (!pl.nv && pl.vec < 8) pl = plan_rows(M, C, type, aligned, pl.vec == 1 ? 8 : 4);
   int nparts = 0;
   rc = with_type(type, [&](auto t) -> int {
     constexpr int T = decltype(t)::value;
@@ -688,6 +693,8 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
       constexpr int VEC = decltype(vec)::value;
       if constexpr (VEC < 8)
         if (pl.nv == 4) return rows(vec, std::integral_constant<int, 4>{});
+      if constexpr (VEC == 1)
+        if (pl.nv == 8) return rows(vec, std::integral_constant<int, 8>{});
       return rows(vec, std::integral_constant<int, 2>{});
     };
     return pl.vec == 1 ? pick(std::integral_constant<int, 1>{}) : pick(std::integral_constant<int, V16>{});
