@@ -184,6 +184,46 @@ norm_round_kernel(const void *h, const float *gain, const float *rstd, int8_t *y
   }
 }
 
+// The same for aligned tensors whose rows are not whole vectors: vectors run over the tensor as one row, and may hold the end of a
+// row and the beginning of the next (C >= VEC).  The elements behind the last vector go to the first block's threads.
+template <int T, int VEC, bool NORM>
+__global__ void __launch_bounds__(ROW_THREADS)
+norm_round_flat_kernel(const void *h, const float *gain, const float *rstd, int8_t *y, int32_t *s_y, const WsHeader *hdr, long long n, int C, Div d_c,
+                       int round_mode) {
+  niti_enter(h, gain, rstd, hdr);
+  const int s = niti_exponent_of(hdr->maxabs32);
+  const float scale = niti_payload_scale(niti_pow2(-s), round_mode);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *s_y = s;
+  const long long items = n / VEC;
+  for (long long i = (long long)(gridDim.x - 1 - blockIdx.x) * ROW_THREADS + threadIdx.x; i < items; i += (long long)gridDim.x * ROW_THREADS) {
+    Pack<T, VEC> p;
+    p.load(h, i * VEC);
+    float v[VEC];
+    if (NORM) {
+      const long long row = d_c.s >= 0 ? (long long)div_by((int)(i * VEC), d_c) : i * VEC / C;
+      const int c = (int)(i * VEC - row * C);
+      const float r0 = rstd[row], r1 = c + VEC > C ? rstd[row + 1] : 0.0f;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) {
+        const bool here = c + j < C;
+        v[j] = p.get(j) * gain[here ? c + j : c + j - C] * (here ? r0 : r1);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) v[j] = p.get(j);
+    }
+    store_payload<VEC, ROUND_BY_ARGUMENT>(y, i * VEC, v, scale, round_mode);
+  }
+  const long long at = items * VEC + threadIdx.x;
+  if (blockIdx.x == 0 && at < n) {
+    Pack<T, 1> p;
+    p.load(h, at);
+    const long long row = at / C;
+    const float v[1] = {NORM ? p.get(0) * gain[at - row * C] * rstd[row] : p.get(0)};
+    store_payload<1, ROUND_BY_ARGUMENT>(y, at, v, scale, round_mode);
+  }
+}
+
 // Rows that are longer than a block's registers: the row is read again (from L2) for the rounding.  2048 x 16384
 // float32 with a residual 109 us, 4.0 TB/s; by single elements 123.
 template <int T, int VEC, bool NORM, bool SHARED>
@@ -580,6 +620,14 @@ int run_norm(niti_ctx *ctx, cudaStream_t st, const NormCall &c, void *ws) {
       else if (c.round_mode == NITI_ROUND_PSR) return second_as(vec, std::integral_constant<int, NITI_ROUND_PSR>{});
       else return second_as(vec, std::integral_constant<int, NITI_ROUND_NEAREST>{});
     };
+    if (aligned && c.C % V16 != 0 && c.C >= V16) {   // (8192 x 4095 bfloat16 15 us, by single elements 95)
+      const long long n = (long long)c.M * c.C, want = (n / V16 + ROW_THREADS - 1) / ROW_THREADS, cap = 8LL * ctx->sm_count;
+      const Div d = n < (1LL << 31) ? make_div(c.C) : Div{0u, -1};
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)(want < cap ? want : cap), ROW_THREADS, 0, norm_round_flat_kernel<T, V16, NORM>, src, c.gain,
+                                     (const float *)rstd, c.y, c.s_y, (const WsHeader *)hdr, n, c.C, d, c.round_mode));
+      ctx->launches++;
+      return NITI_OK;
+    }
     r = aligned && c.C % V16 == 0 ? second(std::integral_constant<int, V16>{}) : second(std::integral_constant<int, 1>{});
     ctx->launches++;
     return r;
