@@ -436,7 +436,8 @@ int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, cons
  * A residual stream of float rows (`type`: NITI_F32, NITI_BF16 or NITI_F16) enters the format through a norm, passes
  * int8 multiplies and comes back through their epilogue.  Float pointers are aligned to their element; rows of whole,
  * 16-byte aligned vectors are fastest.  M = 0 is a valid call.  Sums, statistics and everything between a load and the
- * final rounding are float32.
+ * final rounding are float32.  No call of this section calls the hook of niti_set_reduce_hook(): an exponent for the tensor is
+ * that of this process' rows.
  *
  * Rounding a float y to a payload with exponent s.  For a largest magnitude A the exponent is
  *   s = max(floor(log2 A) - 6, -100),  0 for A = 0,
@@ -469,17 +470,17 @@ int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t *q, int32_t
                   int row_exponents, int round_mode, void *ws, size_t ws_bytes);
 
 /* out[i] = value(q[i]) 2^s[i / per], i < n: payloads (NITI_I8) or codes (NITI_E4M3) of n elements, `per` elements for
- * every exponent (0: one exponent for all); exponents of exponent_bytes = 4 (int32) or 1 (int8). */
+ * every exponent (0: one exponent for all); exponents of exponent_bytes = 4 (int32) or 1 (int8), clamped to -128 .. 127. */
 int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, void *out, int format,
                     int exponent_bytes, int type, int64_t n, int64_t per);
 
 /* Fully connected layer whose result leaves the format in the multiply's epilogue:
  *   z[m][n] = 2^(s_a[m] + s_w) sum_k a[m][k] w[n][k] + bias[n],   out = act(z) + residual.
- * a [M][K] int8 with one exponent per row (row_exponents != 0) or one; w [N][K] int8 with the exponent *s_w; both 16-byte
- * aligned, K <= 131072 (int32 sums are then exact).  bias [N] float32, residual [M][N] may be NULL; out, residual and z
+ * a [M][K] int8 with one exponent per row (row_exponents != 0) or one; w [N][K] int8 with the exponent *s_w; payloads from -127
+ * to 127, both 16-byte aligned, K <= 131072 (int32 sums are then exact).  bias [N] float32, residual [M][N] may be NULL; out, residual and z
  * (NULL unless a backward pass follows) are of `type`; out may be the storage of the residual.  Exponents are clamped, and
- * NITI_DEV_EXP_RANGE raised, where s_a + s_w leaves [-128, 127].  No hook of niti_set_reduce_hook() is called: with
- * exponents per row a row's result depends on nothing else.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
+ * NITI_DEV_EXP_RANGE raised, where s_a + s_w leaves [-128, 127].  With exponents per row a row's result depends on
+ * nothing else.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
 int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, int row_exponents, const int8_t *w,
                         const int32_t *s_w, const float *bias, const void *residual, void *out, void *z, int type, int M,
                         int N, int K, int act, void *ws, size_t ws_bytes);
