@@ -332,6 +332,7 @@ linear_kernel(const __grid_constant__ Maps<N> maps, const __grid_constant__ Laun
       const int slot = tile * CTAS + (int)rank, words = p.bn * BM;
       int *mine = p.slabs + ((long long)slot * p.splits + split) * words + 32 * quarter + lane;
       for (int c = part; c < p.bn / 32; c += EPI_WARPS / 4) {
+        if (row0 >= p.gm || n0 + 32 * c >= p.gn) continue;           // (nobody reads them)
         int v[32];
         tc_ld32(tm + 32u * (unsigned)c, v);
 #pragma unroll
@@ -349,10 +350,11 @@ linear_kernel(const __grid_constant__ Maps<N> maps, const __grid_constant__ Laun
       if (is_last) {
         const int *all = p.slabs + (long long)slot * p.splits * words + 32 * quarter + lane;
         for (int c = part; c < p.bn / 32; c += EPI_WARPS / 4) {
-          if (n0 + 32 * c >= p.gn) continue;
+          if (row0 >= p.gm || n0 + 32 * c >= p.gn) continue;
           int v[32];
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = 0;
+#pragma unroll 2
           for (int k = 0; k < p.splits; ++k) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] += __ldcg(all + (long long)k * words + (32 * c + j) * BM);
