@@ -812,6 +812,20 @@ static int linear_args(niti_ctx *ctx, const char *name, int type, int M, int N, 
   return NITI_OK;
 }
 
+// Are the weights streamed (niti_linear_rows)?  Up to eight rows always; beyond, every block's tokens come through L2 and the sizes
+// from which on the tiles are faster were measured (us, streamed / tiles).  16 rows: 11008 x 4096 13.3 / 18.9, 8192 x 8192 21.1 /
+// 18.9, 16384 x 16384 90 / 54.  32 rows: 4096 x 4096 9.9 / 11.6, 6144 x 4096 16.8 / 12.5, and where not all blocks run at once 8192 x
+// 1024 7.1 / 7.7, 16384 x 1024 12.2 / 8.1.  Rows that are not whole vectors: 16 x 2000 x 2001 10.8 / 12.0, 16 x 8192 x 2001 25 / 20, 32 x
+// 1000 x 777 7.3 / 11.1, 32 x 520 x 3001 22 / 16, 32 x 4096 x 1001 10.6 / 10.9.
+static bool streams(const niti_ctx *ctx, int M, int N, int K) {
+  if (M <= 8) return true;
+  if (M > NITI_LINEAR_ROWS) return false;
+  const long long weights = (long long)N * K, mega = 1 << 20;
+  if (M <= 16) return weights < (K % 16 == 0 ? 48 : 12) * mega;
+  if (K % 16 != 0) return weights < 3 * mega / 2;
+  return weights < (N > 48LL * ctx->sm_count ? 12 : 24) * mega;
+}
+
 extern "C" int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, int row_exponents, const int8_t *w,
                                    const int32_t *s_w, const float *bias, const void *residual, void *out, void *z, int type, int M, int N, int K,
                                    int act, void *ws, size_t ws_bytes) {
@@ -824,7 +838,7 @@ extern "C" int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a,
     return niti_fail(ctx, NITI_ERR_ARG, "niti_linear_act_fwd: bad argument (z has a place of its own; pointers are aligned to their type)");
   cudaStream_t st = (cudaStream_t)stream;
   const LinearEpilogue e = {s_a, s_w, bias, residual, out, z, row_exponents ? 1 : 0, act};
-  if (M <= NITI_LINEAR_ROWS) return niti_linear_rows(ctx, st, a, w, M, N, K, e, type);
+  if (streams(ctx, M, N, K)) return niti_linear_rows(ctx, st, a, w, M, N, K, e, type);
   int8_t *pad = (int8_t *)ws + NITI_WS_HEADER;
   int *slabs = (int *)(pad + pad_bytes(M, K) + pad_bytes(N, K));
   const int pitch = (int)pitch16(K);

@@ -24,6 +24,6 @@ struct LinearMultiply {
 };
 // Words of a zeroed header that count the arrivals of a multiply's split tiles.
 #define NITI_LINEAR_COUNTERS 320
-// The forward multiply of at most NITI_LINEAR_ROWS rows: streams the weights, in the caller's layout whatever K is.
+// The forward multiply of a few rows, at most NITI_LINEAR_ROWS: streams the weights, in the caller's layout whatever K is.
 #define NITI_LINEAR_ROWS 32
 int niti_linear_rows(niti_ctx *ctx, cudaStream_t st, const int8_t *a, const int8_t *w, int M, int N, int K, const LinearEpilogue &e, int type);

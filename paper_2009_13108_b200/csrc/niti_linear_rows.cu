@@ -115,8 +115,8 @@ int niti_linear_rows(niti_ctx *ctx, cudaStream_t st, const int8_t *a, const int8
   };
   // Sixteen warps a block where the contraction feeds them and all blocks still run at once (three an SM), else eight: weights
   // beyond L2, 8 -> 16 warps, 1 x 4096 x 4096 7.5 -> 5.3 us, 32 x 4096 x 4096 13.2 -> 9.9, 1 x 4096 x 16384 25.3 -> 15.4; outside
-  // the rule 1 x 8192 x 4096 9.0 -> 9.2, 16 x 1000 x 512 2.4 -> 2.4.
-  const bool wide = K >= 1024 && (long long)grid <= 3LL * ctx->sm_count;
+  // the rule 1 x 8192 x 4096 9.0 -> 9.2, 16 x 4096 x 1024 3.3 -> 3.9.
+  const bool wide = K >= 2048 && (long long)grid <= 3LL * ctx->sm_count;
   auto go = [&](auto tc, auto nt, auto al) -> int {
     if constexpr (decltype(al)::value)
       if (wide) return go_as(tc, nt, al, std::integral_constant<int, 16>{});

@@ -136,6 +136,19 @@ def test_results_do_not_depend_on_the_other_rows(niti):
         assert torch.equal(part, whole[lo:hi])
 
 
+@pytest.mark.parametrize("M,N,K", [(8, 520, 3001), (9, 4400, 3001), (16, 512, 3001), (17, 600, 3001), (32, 520, 3001), (12, 12304, 4096), (32, 6144, 4096),
+                                   (20, 7136, 2048), (20, 7136, 512)])
+def test_few_rows_of_large_layers(niti, M, N, K):
+    """On both sides of the sizes from which on a few rows go by tiles, and each row as it is alone."""
+    _check_forward(niti, M, N, K, "bf16", "gelu", True, True, True, True)
+    a, w = _i8(1, M, K), _i8(2, N, K)
+    s_a, s_w = _exp(M, True, K), _exp(1, False, K)
+    out, _ = niti.linear_act_fwd(a, s_a, w, s_w, dtype=torch.float32)
+    for m in (0, M - 1):
+        one, _ = niti.linear_act_fwd(a[m:m + 1].clone(), s_a[m:m + 1].clone(), w, s_w, dtype=torch.float32)
+        assert torch.equal(one[0], out[m])
+
+
 def test_rows_behind_the_last_one_stay(niti):
     M, N, K = 37, 100, 64
     a, w, s = _i8(1, M, K), _i8(2, N, K), torch.full((1,), -8, dtype=torch.int32, device="cuda")
