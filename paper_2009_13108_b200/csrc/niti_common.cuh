@@ -114,7 +114,7 @@ __host__ __device__ __forceinline__ unsigned int *niti_split_max(WsHeader *hdr) 
   do {                                                                                  \
     cudaError_t e__ = (expr);                                                           \
     if (e__ != cudaSuccess) {                                                           \
-      snprintf((ctx)->err, sizeof((ctx)->err), "%s failed: %s (%s:%d)", #expr,          \
+      snprintf((ctx)->err, sizeof((ctx)->err), "%.96s failed: %s (%s:%d)", #expr,       \
                cudaGetErrorString(e__), __FILE__, __LINE__);                            \
       return NITI_ERR_CUDA;                                                             \
     }                                                                                   \
