@@ -53,14 +53,23 @@ __device__ __forceinline__ float reciprocal(float x) {
   return r;
 }
 // Roots of two values: the hardware's approximation r and a step of Heron's method, r + (v - r^2) / (2 r), whose residual a fused
-// multiply-add has exactly.  The step squares a relative error of 2^-22, so that what is left decides the rounding only within
-// 2^-20 of a step of a tie: as __fsqrt_rn() (compared by the tests), in half of its instructions.  0 stays 0.
+// multiply-add has exactly as long as r^2 has no bits below 2^-149.  The step squares a relative error of 2^-22, so that what is
+// left decides the rounding only within 2^-20 of a step of a tie: as __fsqrt_rn() (compared by the tests), in half of its
+// instructions.  0 stays 0.  For values of 0 and from SMALL_V on: below it the residual loses bits, and below 2^-126 the
+// approximation is 0.
+constexpr float SMALL_V = 7.888609052210118e-31f;  // 2^-100
 __device__ __forceinline__ F2 root2(float v0, float v1, F2 v) {
   float r0, r1;
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r0) : "f"(v0));
   asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r1) : "f"(v1));
   const F2 r(r0, r1), d = fma2(F2(-r0, -r1), r, v);
   return fma2(d, F2(0.5f * reciprocal(fmaxf(r0, 1e-30f)), 0.5f * reciprocal(fmaxf(r1, 1e-30f))), r);
+}
+// The same for any values, small ones times 2^80 beforehand (exact, and so is the root's way back: it is at least 2^-75).
+__device__ __forceinline__ F2 root2_scaled(float v0, float v1) {
+  const bool s0 = v0 < SMALL_V, s1 = v1 < SMALL_V;
+  const float w0 = s0 ? v0 * 1.2089258196146292e24f : v0, w1 = s1 ? v1 * 1.2089258196146292e24f : v1;
+  return mul2(root2(w0, w1, F2(w0, w1)), F2(s0 ? 9.094947017729282e-13f : 1.0f, s1 ? 9.094947017729282e-13f : 1.0f));
 }
 // In bits 20 .. 27, the code below a magnitude t < 256, given as t 2^-24, plus what 16 random bits (times 16: `sixteen` is 16
 // in a register, which keeps the multiply-add from becoming a shift and an addition on the busier integer pipe) carry into it.
@@ -201,13 +210,22 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
     v[j] = __fadd_rn(__fmul_rn(hy.b2, v[j]), __fmul_rn(__fmul_rn(hy.c2, g[j]), g[j]));
   };
   if (!bad) {
+    float least = TOO_LARGE;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      update(j);
+      least = fminf(least, v[j]);
+    }
+    if (least < SMALL_V) {                         // (zeros, too; rare in a network that learns)
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) root2_scaled(v[j], v[j + 1]).get(r[j], r[j + 1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) root2(v[j], v[j + 1], F2(v[j], v[j + 1])).get(r[j], r[j + 1]);
+    }
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
-      update(j);
-      update(j + 1);
-      const F2 mm(m[j], m[j + 1]), vv(v[j], v[j + 1]);
-      const F2 rr = root2(v[j], v[j + 1], vv);
-      rr.get(r[j], r[j + 1]);
+      const F2 mm(m[j], m[j + 1]), rr(r[j], r[j + 1]);
       float d0, d1;
       fma2(rr, F2(st.den_r), F2(st.den_1)).get(d0, d1);
       fma2(mm, F2(reciprocal(d0), reciprocal(d1)), mul2(F2(p[j], p[j + 1]), F2(st.decay))).get(p[j], p[j + 1]);
