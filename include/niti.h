@@ -515,7 +515,7 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * changes by a thousandth a step would stand still, and one that draws from its own discarded bits does where there is
  * no gradient: the same code times the same constant leaves the same bits.)
  * An element whose scaled gradient is not finite, or 2^63 or more, keeps its weight, m and v, and raises
- * NITI_DEV_NONFINITE. */
+ * NITI_DEV_NONFINITE; so does a weight that is not finite after the step (its int8 copy is +-127). */
 #define NITI_STATE_BLOCK 256
 typedef struct niti_adamw_tensor {
   float *p;

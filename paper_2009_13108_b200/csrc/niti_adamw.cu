@@ -122,7 +122,7 @@ struct Step {                                      // of this step and tensor
 // the integer calls: m mixes a short code and a short gradient with weights 9/10 and 1/10, whose binary expansions repeat the
 // same four bits, and without a gradient a code meets the same constant, and so the same discarded bits, in every step.  A root
 // that is not zero does not round to zero (the next step divides by it).  s_m, s_v: the block's exponents, before and after.
-// Returns whether a gradient was not finite, or too large.
+// Returns whether a gradient was not finite, or too large, or a weight is not finite now.
 // VEC: the operands are in shared memory at `stage` (the barrier `empty` is told when they have been read), else everything
 // goes by elements.
 template <bool EIGHT, bool VEC>
@@ -239,6 +239,9 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
       if (ok) p[j] = fmaf(m[j], reciprocal(fmaf(r[j], st.den_r, st.den_1)), p[j] * st.decay);
     }
   }
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = niti_absmax(top, p[j]);
   if (EIGHT) {
     float am = 0.0f, ar = 0.0f, lm = fabsf(m[0]), lr = r[0];
 #pragma unroll
@@ -310,7 +313,7 @@ __device__ __forceinline__ bool adamw_block(const Tensor &T, const Hyper &hy, co
       if (T.w8) T.w8[e] = (int8_t)niti_payload<false>(p[j], st.w_scale);
     }
   }
-  return bad;
+  return bad || !(top < __int_as_float(0x7f800000));
 }
 
 __device__ __forceinline__ void bulk_load(unsigned dst, const void *src, unsigned bytes, unsigned bar) {

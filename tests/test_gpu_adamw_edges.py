@@ -1,4 +1,4 @@
-"""AdamW where its numbers are at the ends of float32: second moments that are subnormal."""
+"""AdamW where its numbers are at the ends of float32: second moments that are subnormal, weights that are not finite."""
 import numpy as np
 import pytest
 import torch
@@ -104,3 +104,28 @@ def test_elements_do_not_depend_on_their_neighbours_gradients(niti, bits):
     keep[5::64] = False
     for a, b in zip(*runs):
         assert torch.equal(a[keep], b[keep])
+
+
+@pytest.mark.parametrize("w8", [False, True])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("n,at", [(2048 * 3, 2048 + 77), (300, 299)])
+def test_weights_that_are_not_finite_raise_the_status(niti, bits, w8, n, at):
+    from paper_2009_13108_b200 import NitiError
+    for x in (float("inf"), float("-inf"), float("nan")):
+        p = torch.from_numpy((0.05 * np.random.default_rng(8).standard_normal(n)).astype(F)).cuda()
+        g = torch.from_numpy(_gradients(n, 9, -4.0, -2.0)).cuda()
+        m, v, s_m, s_v = niti.adamw_state(p, bits)
+        w = torch.zeros(n, dtype=torch.int8, device="cuda")
+        plan = niti.adamw_tensors([p], [g], [m], [v], s_m=[s_m] if bits == 8 else None, s_v=[s_v] if bits == 8 else None,
+                                  w8=[w] if w8 else None, s_w=[niti.scalar(-9)] if w8 else None)
+        niti.adamw(plan, _step(1), LR)
+        assert niti.check() == 0
+        p[at] = x
+        niti.adamw(plan, _step(2), LR)
+        with pytest.raises(NitiError, match="0x40|64|status"):
+            niti.check()
+        rest = torch.ones(n, dtype=torch.bool)
+        rest[at] = False
+        assert torch.isfinite(p[rest]).all() and not torch.isfinite(p[at])
+        if w8:
+            assert abs(int(w[at])) == 127
