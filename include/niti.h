@@ -497,7 +497,8 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
                         int dw_type, int M, int N, int K, int act, int round_mode, void *ws, size_t ws_bytes);
 
 /* One AdamW step over n tensors (a host array that the call reads before it returns; two of them must not share
- * memory).  0 <= lr, weight_decay <= 1e6, 0 <= beta < 1, 1e-20 <= eps <= 1e6.  With t = *step, the number of this step
+ * memory).  0 <= lr, weight_decay <= 1e6, 0 <= beta < 1, 1e-20 <= eps <= 1e6; where lr / (1 - beta1^t) is below 1e-30 the
+ * states move and the weights only decay.  With t = *step, the number of this step
  * (device int32, >= 1: a captured graph counts it up between its replays), and g the gradient times *grad_scale (device
  * float32, NULL: 1):
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,

@@ -389,11 +389,11 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
   }
   Step st;
   // 1 - b^t without its cancellation
-  // (a learning rate of 0 becomes a step of nothing; with the bounds that the call puts on lr and eps every denominator is
-  // finite and not 0, so that an element without a gradient does not become 0 / 0 or 0 times infinity)
-  const float lr = fmaxf(hy.lr / -expm1f((float)t_step * hy.log_b1), 1e-30f);
+  // (with the bounds that the call puts on lr and eps every denominator is finite and not 0, so that an element without a
+  // gradient does not become 0 / 0 or 0 times infinity; a learning rate of 0 has infinite ones, whose reciprocals are 0)
+  const float lr_t = hy.lr / -expm1f((float)t_step * hy.log_b1), lr = fmaxf(lr_t, 1e-30f);
   st.den_r = -rsqrtf(-expm1f((float)t_step * hy.log_b2)) / lr;
-  st.den_1 = -fmaxf(hy.eps / lr, 1e-37f);          // (its reciprocal is finite)
+  st.den_1 = lr_t < 1e-30f ? __int_as_float(0xff800000) : -fmaxf(hy.eps / lr, 1e-37f);          // (its reciprocal is finite)
   st.gs = grad_scale ? *grad_scale : 1.0f;
   st.scaled = grad_scale != nullptr;
   st.key = (unsigned)t_step * 0x9E3779B9u;
