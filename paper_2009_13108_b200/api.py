@@ -683,8 +683,8 @@ class Niti:
         return out, z
 
     def linear_act_bwd(self, a, s_a, w, s_w, dout, z=None, act="none", need_dx=True, dx=None, dw=None, dbias=None,
-                       dw_dtype=torch.float32, round_mode=ROUND_NEAREST):
-        """niti_linear_act_bwd: (dx, dw, dbias); dx is None unless ``need_dx``.  a has one exponent."""
+                       dw_dtype=torch.float32, round_mode=ROUND_NEAREST, need_dw=True, need_dbias=True):
+        """niti_linear_act_bwd: (dx, dw, dbias), each None unless it is needed.  a has one exponent."""
         type_id = self._float(dout, "dout")
         M, N = dout.shape
         if act not in _ACTS or dw_dtype not in _TYPES or a.dim() != 2:
@@ -696,9 +696,12 @@ class Niti:
         self._tensor(s_w, "s_w", (1,), torch.int32)
         if z is not None:
             self._tensor(z, "z", dout.shape, dout.dtype)
+        for name, need, given in (("dx", need_dx, dx), ("dw", need_dw, dw), ("dbias", need_dbias, dbias)):
+            if given is not None and not need:
+                raise NitiError(ERR_ARG, "linear_act_bwd: a tensor for %s, which is not needed" % name)
         dx = self._out(dx, "dx", (M, K), dout.dtype) if need_dx else None
-        dw = self._out(dw, "dw", (N, K), dw_dtype)
-        dbias = self._out(dbias, "dbias", (N,), torch.float32)
+        dw = self._out(dw, "dw", (N, K), dw_dtype) if need_dw else None
+        dbias = self._out(dbias, "dbias", (N,), torch.float32) if need_dbias else None
         ws, wsb = self._ws_for(OP_LINEAR_ACT_BWD, M, N, K)
         self._ck(self.lib.niti_linear_act_bwd(self.h, self._stream(), _ptr(a), _ptr(s_a), _ptr(w), _ptr(s_w), _ptr(z), _ptr(dout),
                                               _ptr(dx), _ptr(dw), _ptr(dbias), type_id, _TYPES[dw_dtype], M, N, K, _ACTS[act],

@@ -740,6 +740,19 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
   if ((threadIdx.x & 31) == 0 && most) atomicMax(&hdr->maxabs32, most);
 }
 
+// The bias gradient of 32 columns from the row blocks' column sums.
+__device__ __forceinline__ void bias_sums(const float *part, float *dbias, int nblk, int N, int block) {
+  __shared__ float buf[16 * 33];
+  if (N % 4 == 0) niti_column_sums<4, 16>(part, dbias, nblk, N, block, buf);
+  else niti_column_sums<1, 4>(part, dbias, nblk, N, block, buf);
+}
+// Where no multiply follows; the order of the sums is the same.
+__global__ void __launch_bounds__(ERR_THREADS)
+bias_sum_kernel(const float *part, float *dbias, int nblk, int N) {
+  niti_enter(part);
+  bias_sums(part, dbias, nblk, N, (int)blockIdx.x);
+}
+
 // e as payload with the exponent of its maximum, rows of `pitch` bytes.  The rows that the pass before read last come first.
 // Beside it, the bias gradient from that pass' column sums (of `nblk` row blocks).
 template <int T, int VEC, int ACT, bool PSR>
@@ -755,9 +768,7 @@ error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, co
     if (most >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
   }
   if ((int)blockIdx.x >= g.main) {
-    __shared__ float buf[16 * 33];
-    if (N % 4 == 0) niti_column_sums<4, 16>(part, dbias, nblk, N, (int)blockIdx.x - g.main, buf);
-    else niti_column_sums<1, 4>(part, dbias, nblk, N, (int)blockIdx.x - g.main, buf);
+    bias_sums(part, dbias, nblk, N, (int)blockIdx.x - g.main);
     return;
   }
   const int b = g.main - 1 - (int)blockIdx.x, by = b / g.strips, bx = b - by * g.strips;
@@ -782,7 +793,6 @@ int error_blocks(long long M, long long N) {
 }  // namespace
 
 int niti_launch_pad_pitch2(niti_ctx *ctx, cudaStream_t st, const PadJob &a, const PadJob &b);
-int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C);
 
 size_t niti_linear_act_ws_bytes(int op, long long M, long long N, long long K) {
   size_t b = NITI_WS_HEADER + pad_bytes(M, K) + pad_bytes(N, K) + (size_t)NITI_LINEAR_MAX_SMS * BM * 256 * 4;
@@ -902,7 +912,11 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
                                    dbias ? part : (float *)nullptr, hdr, next, M, N, g, job_w, job_a, pad0));
     ctx->launches++;
     niti_header_passed_on(ctx, next);
-    if (!dx && !dw) return niti_launch_column_sums(ctx, st, part, dbias, blocks, N);
+    if (!dx && !dw) {
+      NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)((N + 31) / 32), ERR_THREADS, 0, bias_sum_kernel, (const float *)part, dbias, blocks, N));
+      ctx->launches++;
+      return NITI_OK;
+    }
     auto second = [&](auto psr) -> int {
       const unsigned extra = dbias ? (unsigned)((N + 31) / 32) : 0u;
       NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)g.main + extra, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT, decltype(psr)::value>, dout, z, e8, s_e,

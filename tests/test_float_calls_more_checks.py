@@ -1,0 +1,23 @@
+"""More of what the binding of the float-side calls refuses, and what it hands to the library (CPU: the library is replaced by one
+that records calls)."""
+import pytest
+import torch
+
+from test_float_calls_checks import _ran, niti            # noqa: F401  (the fixture)
+
+BF = torch.bfloat16
+
+
+def test_parts_of_the_backward_call(niti):                          # noqa: F811
+    a, w, s = torch.zeros(3, 16, dtype=torch.int8), torch.zeros(5, 16, dtype=torch.int8), torch.zeros(1, dtype=torch.int32)
+    d = torch.zeros(3, 5, dtype=BF)
+    for x in (False, True):
+        for y in (False, True):
+            for b in (False, True):
+                got = niti.linear_act_bwd(a, s, w, s, d, need_dx=x, need_dw=y, need_dbias=b)
+                args = _ran(niti, "niti_linear_act_bwd")[-1]
+                assert [g is not None for g in got] == [p is not None for p in args[8:11]] == [x, y, b]
+    from paper_2009_13108_b200 import NitiError
+    for kw in (dict(dx=torch.zeros(3, 16, dtype=BF), need_dx=False), dict(dw=torch.zeros(5, 16), need_dw=False), dict(dbias=torch.zeros(5), need_dbias=False)):
+        with pytest.raises(NitiError):
+            niti.linear_act_bwd(a, s, w, s, d, **kw)
