@@ -707,8 +707,8 @@ struct ErrorGrid { int strips, rows, main; };
 // bytes as both operands.
 template <int T, int VEC, int ACT>
 __global__ void __launch_bounds__(ERR_THREADS, 8)
-error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, int M, int N, ErrorGrid g, PadJob pad0, PadJob pad1,
-                 unsigned pad0_blocks) {
+error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, WsHeader *next, uint32_t *status, int M, int N, ErrorGrid g,
+                 PadJob pad0, PadJob pad1, unsigned pad0_blocks) {
   niti_enter(dout, z, pad0.src, pad1.src);
   if ((int)blockIdx.x >= g.main) {
     const unsigned b = blockIdx.x - (unsigned)g.main, all = gridDim.x - (unsigned)g.main;
@@ -738,6 +738,7 @@ error_max_kernel(const void *dout, const void *z, float *part, WsHeader *hdr, Ws
   }
   const unsigned most = __reduce_max_sync(0xffffffffu, __float_as_uint(largest));
   if ((threadIdx.x & 31) == 0 && most) atomicMax(&hdr->maxabs32, most);
+  if ((threadIdx.x & 31) == 0 && most >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
 }
 
 // The bias gradient of 32 columns from the row blocks' column sums.
@@ -757,16 +758,13 @@ bias_sum_kernel(const float *part, float *dbias, int nblk, int N) {
 // Beside it, the bias gradient from that pass' column sums (of `nblk` row blocks).
 template <int T, int VEC, int ACT, bool PSR>
 __global__ void __launch_bounds__(ERR_THREADS, 8)
-error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, uint32_t *status, int M, int N, ErrorGrid g,
-                   int pitch, const float *part, float *dbias, int nblk) {
+error_round_kernel(const void *dout, const void *z, int8_t *e8, int32_t *s_e, const WsHeader *hdr, int M, int N, ErrorGrid g, int pitch,
+                   const float *part, float *dbias, int nblk) {
   niti_enter(dout, z, hdr, part);
   const unsigned most = hdr->maxabs32;
   const int s = niti_exponent_of(most);
   const float scale = niti_payload_scale(niti_pow2(-s), PSR ? NITI_ROUND_PSR : NITI_ROUND_NEAREST);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    *s_e = s;
-    if (most >= INF_BITS) atomicOr(status, NITI_DEV_NONFINITE);
-  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *s_e = s;
   if ((int)blockIdx.x >= g.main) {
     bias_sums(part, dbias, nblk, N, (int)blockIdx.x - g.main);
     return;
@@ -909,7 +907,7 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
     g.rows = rows;
     g.main = g.strips * blocks;
     NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)g.main + pad0 + pad1, ERR_THREADS, 0, error_max_kernel<T, VEC, ACT>, dout, z,
-                                   dbias ? part : (float *)nullptr, hdr, next, M, N, g, job_w, job_a, pad0));
+                                   dbias ? part : (float *)nullptr, hdr, next, ctx->d_status, M, N, g, job_w, job_a, pad0));
     ctx->launches++;
     niti_header_passed_on(ctx, next);
     if (!dx && !dw) {
@@ -920,7 +918,7 @@ extern "C" int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a,
     auto second = [&](auto psr) -> int {
       const unsigned extra = dbias ? (unsigned)((N + 31) / 32) : 0u;
       NITI_CUDA_TRY(ctx, niti_launch(st, (unsigned)g.main + extra, ERR_THREADS, 0, error_round_kernel<T, VEC, ACT, decltype(psr)::value>, dout, z, e8, s_e,
-                                     (const WsHeader *)hdr, ctx->d_status, M, N, g, pitch_e, (const float *)part, dbias, blocks));
+                                     (const WsHeader *)hdr, M, N, g, pitch_e, (const float *)part, dbias, blocks));
       ctx->launches++;
       return NITI_OK;
     };
