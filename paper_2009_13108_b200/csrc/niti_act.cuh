@@ -18,32 +18,48 @@ __device__ __forceinline__ float fast_reciprocal(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
-// Phi of two values, and exp(-z^2 / 2).  For a = |z|: 1 - Phi(a) = t (a1 + t (a2 + ...)) exp(-a^2 / 2) / 2 with t = 1 / (1 + p a /
-// sqrt 2), Abramowitz and Stegun 7.1.26 (error of erf at most 1.5e-7, of Phi half of that).  Phi(z) = 1/2 + sign(z) (1/2 - that).
-__device__ __forceinline__ F2 normal_cdf2(float z0, float z1, F2 z, F2 &g) {
+// b = -|z|, not below -40 (there the tail is 0: no product with an infinity), NaN for NaN
+__device__ __forceinline__ float minus_magnitude(float z) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(-fabsf(z)), "f"(-40.0f));
+  return r;
+}
+// The normal distribution's tail of two values -b >= 0: Q = 1 - Phi(-b) as q g with g = exp(-b^2 / 2).  q = Q exp(b^2 / 2) falls
+// slowly: with t = 1 / (1 - 0.265 b), q / t is a polynomial of degree 8 in b t, fitted on [0, 14] for the least relative error
+// (1.3e-8) with the value 1/2 at 0.  Relative to Q that leaves what reciprocal, exponential and roundings cost, at most 5 2^-22, and
+// the rounding of the exponent, b^2 2^-23.7 (measured 2.4e-7 up to 1, 5.4e-7 up to 3, 1.6e-6 up to 6).  Phi of a negative
+// argument is Q itself: 1 - (1 - Q) would leave no digits of a small tail.  (A shorter polynomial that only kept the absolute error
+// below 1e-7 took 6 us less of the two error passes of 4096 x 4096.)
+__device__ __forceinline__ F2 normal_tail2(F2 b, F2 &g) {
   float d0, d1, x0, x1;
-  fma2(F2(fabsf(z0), fabsf(z1)), F2(0.3275911f * 0.70710678f), F2(1.0f)).get(d0, d1);
-  mul2(mul2(z, F2(-0.72134752f)), z).get(x0, x1);
-  const F2 t(fast_reciprocal(d0), fast_reciprocal(d1));
+  fma2(b, F2(-0.265f), F2(1.0f)).get(d0, d1);
+  mul2(mul2(b, F2(-0.72134752f)), b).get(x0, x1);
+  const F2 t(fast_reciprocal(d0), fast_reciprocal(d1)), s = mul2(b, t);
   g = F2(fast_exp2(x0), fast_exp2(x1));
-  F2 q = fma2(t, F2(-0.5f * 1.061405429f), F2(0.5f * 1.453152027f));
-  q = fma2(t, q, F2(-0.5f * 1.421413741f));
-  q = fma2(t, q, F2(0.5f * 0.284496736f));
-  q = fma2(t, q, F2(-0.5f * 0.254829592f));
-  float h0, h1;                                    // 1/2 - tail
-  fma2(mul2(q, t), g, F2(0.5f)).get(h0, h1);
-  return add2(F2(copysignf(h0, z0), copysignf(h1, z1)), F2(0.5f));
+  F2 q = fma2(s, F2(7.47861634e-07f), F2(9.37091863e-06f));
+  q = fma2(s, q, F2(2.45498723e-05f));
+  q = fma2(s, q, F2(-0.000147059225f));
+  q = fma2(s, q, F2(-0.000331738207f));
+  q = fma2(s, q, F2(0.00898367632f));
+  q = fma2(s, q, F2(0.0736756772f));
+  q = fma2(s, q, F2(0.266442508f));
+  q = fma2(s, q, F2(0.5f));
+  return mul2(q, t);
 }
+// z Phi(z) = max(z, 0) - |z| Q(|z|)
 __device__ __forceinline__ F2 gelu2(float z0, float z1) {
-  const F2 z(z0, z1);
+  const F2 b(minus_magnitude(z0), minus_magnitude(z1));
   F2 g(0.0f);
-  return mul2(z, normal_cdf2(z0, z1, z, g));
+  const F2 q = normal_tail2(b, g);
+  return fma2(b, mul2(q, g), F2(fmaxf(z0, 0.0f), fmaxf(z1, 0.0f)));
 }
+// Phi(z) + z phi(z): for negative z u = Q(|z|) - |z| phi(z), for others 1 - u: k u + (1 - k) / 2 with k = 1 or -1
 __device__ __forceinline__ F2 gelu_slope2(float z0, float z1) {
-  const F2 z(z0, z1);
+  const F2 b(minus_magnitude(z0), minus_magnitude(z1));
   F2 g(0.0f);
-  const F2 cdf = normal_cdf2(z0, z1, z, g);
-  return fma2(mul2(z, F2(0.3989422804f)), g, cdf);
+  const F2 q = normal_tail2(b, g);
+  const F2 u = mul2(fma2(b, F2(0.3989422804f), q), g), k(copysignf(1.0f, -z0), copysignf(1.0f, -z1));
+  return fma2(u, k, fma2(k, F2(-0.5f), F2(0.5f)));
 }
 __device__ __forceinline__ float gelu(float z) {
   float a, b;
