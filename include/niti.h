@@ -481,7 +481,7 @@ int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, v
  * (NULL unless a backward pass follows) are of `type`; out may be the storage of the residual.  Exponents are clamped, and
  * NITI_DEV_EXP_RANGE raised, where s_a + s_w leaves [-128, 127].  With exponents per row a row's result depends on
  * nothing else.  GELU is max(z, 0) - |z| Q(|z|), the tail Q of the normal distribution being off by at most 2^-19 + z^2 2^-23 of
- * itself; at infinite z it has its limits.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
+ * itself, SiLU by 2^-21; at infinite z both have their limits.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
 int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, int row_exponents, const int8_t *w,
                         const int32_t *s_w, const float *bias, const void *residual, void *out, void *z, int type, int M,
                         int N, int K, int act, void *ws, size_t ws_bytes);

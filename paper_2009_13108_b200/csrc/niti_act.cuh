@@ -71,11 +71,46 @@ __device__ __forceinline__ float gelu_slope(float z) {
   gelu_slope2(z, z).get(a, b);
   return a;
 }
-__device__ __forceinline__ float sigmoid(float z) { return fast_reciprocal(1.0f + fast_exp2(z * -1.44269504f)); }
-__device__ __forceinline__ float silu(float z) { return z * sigmoid(z); }
+constexpr float LOG2E_REST = 1.92596299e-08f;              // log2 e less its float32
+// Beyond +-150 the sigmoid is 0 or 1; NaN for NaN
+__device__ __forceinline__ float at_least_m150(float z) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(-150.0f));
+  return r;
+}
+__device__ __forceinline__ float at_most_150(float z) {
+  float r;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(z), "f"(150.0f));
+  return r;
+}
+// Sigmoids of two values between these: 1 / (1 + 2^x) for x = -z log2 e rounded, corrected for what x misses by, of which a multiply-add
+// has all but the error of log2 e: s' = -s (1 - s), against a relative error of |z| 2^-24.  Within 2^-21 of themselves.
+__device__ __forceinline__ F2 sigmoid2(F2 z) {
+  const F2 n = mul2(z, F2(1.44269504f)), miss = fma2(z, F2(-1.44269504f), n);       // -x, and by how much x is too small
+  float n0, n1, d0, d1;
+  n.get(n0, n1);
+  add2(F2(fast_exp2(-n0), fast_exp2(-n1)), F2(1.0f)).get(d0, d1);
+  const F2 s(fast_reciprocal(d0), fast_reciprocal(d1));
+  return fma2(mul2(s, add2(s, F2(-1.0f))), fma2(z, F2(-LOG2E_REST * 0.69314718f), mul2(miss, F2(0.69314718f))), s);
+}
+__device__ __forceinline__ F2 silu2(float z0, float z1) {
+  const float a0 = at_least_m150(z0), a1 = at_least_m150(z1);
+  return mul2(F2(a0, a1), sigmoid2(F2(at_most_150(a0), at_most_150(a1))));
+}
+// s (1 + z (1 - s))
+__device__ __forceinline__ F2 silu_slope2(float z0, float z1) {
+  const F2 z(at_most_150(at_least_m150(z0)), at_most_150(at_least_m150(z1))), s = sigmoid2(z);
+  return mul2(s, fma2(z, fma2(s, F2(-1.0f), F2(1.0f)), F2(1.0f)));
+}
+__device__ __forceinline__ float silu(float z) {
+  float a, b;
+  silu2(z, z).get(a, b);
+  return a;
+}
 __device__ __forceinline__ float silu_slope(float z) {
-  const float s = sigmoid(z);
-  return s * fmaf(z, 1.0f - s, 1.0f);
+  float a, b;
+  silu_slope2(z, z).get(a, b);
+  return a;
 }
 __device__ __forceinline__ float act_one(float z, int act) {
   switch (act) {
@@ -99,6 +134,9 @@ __device__ __forceinline__ void act_backward(const float (&d)[N], const float (&
   if constexpr (ACT == NITI_ACT_GELU && N % 2 == 0) {
 #pragma unroll
     for (int j = 0; j < N; j += 2) mul2(F2(d[j], d[j + 1]), gelu_slope2(z[j], z[j + 1])).get(e[j], e[j + 1]);
+  } else if constexpr (ACT == NITI_ACT_SILU && N % 2 == 0) {
+#pragma unroll
+    for (int j = 0; j < N; j += 2) mul2(F2(d[j], d[j + 1]), silu_slope2(z[j], z[j + 1])).get(e[j], e[j + 1]);
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j) e[j] = d[j] * act_slope(z[j], ACT);
@@ -118,7 +156,7 @@ __device__ __forceinline__ void act_all(float (&x)[N], int act) {
       break;
     case NITI_ACT_SILU:
 #pragma unroll
-      for (int j = 0; j < N; ++j) x[j] = silu(x[j]);
+      for (int j = 0; j + 1 < N; j += 2) silu2(x[j], x[j + 1]).get(x[j], x[j + 1]);
       break;
     default: break;
   }

@@ -1,10 +1,10 @@
-"""GELU and its slope in float32 over their whole range, against 64 bits.  The argument is a bias beside sums of zeros, so
+"""GELU, SiLU and their slopes in float32 over their whole range, against 64 bits.  The argument is a bias beside sums of zeros, so
 that it is exact; the slope is the bias gradient of one row with an error of one.
 
 Bounds.  With a = |z|, Q the tail of the normal distribution, GELU is max(z, 0) - a Q(a).  The tail takes one reciprocal (2^-23)
 and one exponential (2^-22), a polynomial whose argument carries the reciprocal's error and the rounding of two operations
 (2^-22, which moves it by no more than as much), its own roundings and fit (2^-23), and two products: below 5 * 2^-22.  The
-exponent z^2 / 2 is rounded twice, and its factor once: z^2 2^-23.7."""
+exponent z^2 / 2 is rounded twice, and its factor once: z^2 2^-23.7.  SiLU: exponential, reciprocal and five roundings, below 2^-21."""
 import numpy as np
 import pytest
 import torch
@@ -60,6 +60,14 @@ def test_gelu(niti, M, N):
     assert np.all(np.abs(got - want) <= (TAIL + z * z * 2.0 ** -23) * part + STEP * np.abs(want) + LEAST)
 
 
+@pytest.mark.parametrize("M,N", [(1, 16384), (200, 4096), (200, 4095)])
+def test_silu(niti, M, N):
+    z = _points(N)
+    got, z = _forward(niti, z, "silu", M), z.astype(float)
+    want = z * torch.sigmoid(torch.from_numpy(z)).numpy()
+    assert np.all(np.abs(got - want) <= 2.0 ** -21 * np.abs(want) + LEAST)
+
+
 @pytest.mark.parametrize("N", [16384, 4095])
 def test_gelu_slope(niti, N):
     """u = phi(a) a - Q(a): 1 + u, or -u for negative z."""
@@ -71,7 +79,18 @@ def test_gelu_slope(niti, N):
     assert np.all(np.abs(got - want) <= off + 2 * STEP * np.abs(want) + LEAST)
 
 
-@pytest.mark.parametrize("act", ["gelu"])
+@pytest.mark.parametrize("N", [16384, 4095])
+def test_silu_slope(niti, N):
+    """s (1 + z (1 - s)): s is off by 2^-21 of itself, 1 - s by that of s and half a step."""
+    z = _points(N)
+    got, z = _slope(niti, z, "silu"), z.astype(float)
+    s, t = torch.sigmoid(torch.from_numpy(z)).numpy(), torch.sigmoid(torch.from_numpy(-z)).numpy()
+    want = s * (1 + z * t)
+    off = s * (2.0 ** -21 * (np.abs(1 + z * t) + np.abs(z) * s) + 3 * STEP * (1 + np.abs(z) * t) + STEP * np.abs(z))
+    assert np.all(np.abs(got - want) <= off + LEAST)
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
 def test_arguments_that_are_not_finite(niti, act):
     """The limits at both ends, and NaN for NaN."""
     z = np.array([np.inf, -np.inf, np.nan, 3e38, -3e38, 1.0, -1.0, 0.0], dtype=np.float32)
