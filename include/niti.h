@@ -435,7 +435,7 @@ int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, cons
 /* ---- Float tensors at the boundary of the format: the feed-forward block of a transformer --------------------------
  * A residual stream of float rows (`type`: NITI_F32, NITI_BF16 or NITI_F16) enters the format through a norm, passes
  * int8 multiplies and comes back through their epilogue.  Float pointers are aligned to their element; rows of whole,
- * 16-byte aligned vectors are fastest.  M = 0 is a valid call.  Sums, statistics and everything between a load and the
+ * 16-byte aligned vectors are fastest.  M = 0 is a valid call (one exponent for the tensor is 0 then).  Sums, statistics and everything between a load and the
  * final rounding are float32.  No call of this section calls the hook of niti_set_reduce_hook(): an exponent for the tensor is
  * that of this process' rows.
  *

@@ -656,12 +656,21 @@ static int norm_args(niti_ctx *ctx, const char *name, int type, int M, int C, vo
   return NITI_OK;
 }
 
+// A tensor without rows has the exponent of one of zeros.
+static int exponent_of_nothing(niti_ctx *ctx, void *stream, int32_t *s, int row_exponents) {
+  if (row_exponents || !s) return NITI_OK;
+  if (misaligned(s, 4)) return niti_fail(ctx, NITI_ERR_ARG, "bad argument (pointers are aligned to their type)");
+  NITI_CUDA_TRY(ctx, cudaMemsetAsync(s, 0, 4, (cudaStream_t)stream));
+  return NITI_OK;
+}
+
 extern "C" int niti_rmsnorm_fwd(niti_ctx *ctx, void *stream, const void *x, const void *residual, const float *gain, void *h, int8_t *y,
                                 int32_t *s_y, float *rstd, int type, int M, int C, int row_exponents, float eps, int round_mode, void *ws,
                                 size_t ws_bytes) {
   if (!ctx) return NITI_ERR_ARG;
   const int rc = norm_args(ctx, "niti_rmsnorm_fwd", type, M, C, ws, ws_bytes, NITI_OP_RMSNORM_FWD);
-  if (rc != NITI_OK || M == 0) return rc;
+  if (rc != NITI_OK) return rc;
+  if (M == 0) return exponent_of_nothing(ctx, stream, s_y, row_exponents);
   const uintptr_t es = (uintptr_t)niti_type_size(type);
   if (!x || !gain || !y || !s_y || (residual && !h) || !(eps >= 0.0f) || (round_mode != NITI_ROUND_PSR && round_mode != NITI_ROUND_NEAREST) ||
       (((uintptr_t)x | (uintptr_t)residual | (uintptr_t)h) & (es - 1)) || (((uintptr_t)gain | (uintptr_t)s_y | (uintptr_t)rstd) & 3))
@@ -674,7 +683,8 @@ extern "C" int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t 
                              int round_mode, void *ws, size_t ws_bytes) {
   if (!ctx) return NITI_ERR_ARG;
   const int rc = norm_args(ctx, "niti_quantize", type, M, C, ws, ws_bytes, NITI_OP_QUANTIZE);
-  if (rc != NITI_OK || M == 0) return rc;
+  if (rc != NITI_OK) return rc;
+  if (M == 0) return exponent_of_nothing(ctx, stream, s, row_exponents);
   if (!x || !q || !s || misaligned(x, (uintptr_t)niti_type_size(type)) || misaligned(s, 4) ||
       (round_mode != NITI_ROUND_PSR && round_mode != NITI_ROUND_NEAREST))
     return niti_fail(ctx, NITI_ERR_ARG, "niti_quantize: bad argument (pointers are aligned to their type)");
@@ -684,7 +694,7 @@ extern "C" int niti_quantize(niti_ctx *ctx, void *stream, const void *x, int8_t 
   return run_norm<false>(ctx, (cudaStream_t)stream, c, ws);
 }
 
-int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C);
+static int launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C);
 
 extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, const void *h, const float *gain, const float *rstd, const void *dh,
                                 void *dx, float *dgain, int type, int M, int C, void *ws, size_t ws_bytes) {
@@ -749,11 +759,11 @@ extern "C" int niti_rmsnorm_bwd(niti_ctx *ctx, void *stream, const void *dy, con
   });
   ctx->launches++;
   if (rc != NITI_OK || !dgain) return rc;
-  return niti_launch_column_sums(ctx, st, part, dgain, nparts, C);
+  return launch_column_sums(ctx, st, part, dgain, nparts, C);
 }
 
 // dst[c] = sum over n rows of part[n][C], in a fixed order
-int niti_launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C) {
+static int launch_column_sums(niti_ctx *ctx, cudaStream_t st, const float *part, float *dst, int n, int C) {
   const unsigned grid = (unsigned)((C + 31) / 32);
   if (C % 4 == 0) NITI_CUDA_TRY(ctx, niti_launch(st, grid, 256, 0, column_sum_kernel<4>, part, dst, n, C));
   else NITI_CUDA_TRY(ctx, niti_launch(st, grid, 1024, 0, column_sum_kernel<1>, part, dst, n, C));
