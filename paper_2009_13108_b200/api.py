@@ -564,6 +564,12 @@ class Niti:
         raise NitiError(ERR_ARG, "%s: a contiguous tensor on %s is needed, %s %s; got %s %s on %s" % (
             name, self.device, dtype or "of a type that the call takes", "" if shape is None else tuple(shape), t.dtype, tuple(t.shape), t.device))
 
+    def _scalar(self, t, name, dtype):
+        """A device scalar, or NitiError.  (An empty tensor's pointer is null, which the library takes for none given.)"""
+        if t.numel() < 1:
+            raise NitiError(ERR_ARG, "%s: a tensor with an element is needed" % name)
+        return self._tensor(t, name, None, dtype)
+
     def _float(self, t, name):
         """(type id) of an activation tensor."""
         type_id = _TYPES.get(t.dtype)
@@ -662,8 +668,8 @@ class Niti:
         """niti_linear_act_fwd: (out, z); z, the argument of the activation, is None unless ``keep_z`` (or a tensor for it) is
         given.  ``s_a``: [M] exponents, or [1]; ``act``: "none", "relu", "gelu" or "silu"."""
         self._tensor(a, "a", None, torch.int8)
-        if a.dim() != 2 or act not in _ACTS or dtype not in _TYPES:
-            raise NitiError(ERR_ARG, "linear_act_fwd: a matrix, a known activation and a float type are needed")
+        if a.dim() != 2 or w.dim() != 2 or act not in _ACTS or dtype not in _TYPES:
+            raise NitiError(ERR_ARG, "linear_act_fwd: two matrices, a known activation and a float type are needed")
         M, K = a.shape
         N = w.shape[0]
         self._tensor(w, "w", (N, K), torch.int8)
@@ -744,16 +750,16 @@ class Niti:
                 self._tensor(sv, name + "s_v", blocks, torch.int8)
             if w is not None:
                 self._tensor(w, name + "w8", p.shape, torch.int8)
-                self._tensor(sw, name + "s_w", None, torch.int32)
+                self._scalar(sw, name + "s_w", torch.int32)
             array[i] = _AdamwTensor(_ptr(p), _ptr(g), _ptr(mi), _ptr(vi), _ptr(sm), _ptr(sv), _ptr(w), _ptr(sw), p.numel(),
                                     decay[i], _TYPES[g.dtype])
         return AdamwTensors(array, 8 if eight else 32, [list(params)] + lists)
 
     def adamw(self, tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):
         """niti_adamw on a list of ``adamw_tensors``; ``step``: device int32 scalar, the number of this step (from 1)."""
-        self._tensor(step, "step", None, torch.int32)
+        self._scalar(step, "step", torch.int32)
         if grad_scale is not None:
-            self._tensor(grad_scale, "grad_scale", None, torch.float32)
+            self._scalar(grad_scale, "grad_scale", torch.float32)
         self._ck(self.lib.niti_adamw(self.h, self._stream(), tensors.array, len(tensors), tensors.state_bits, _ptr(step), lr,
                                      betas[0], betas[1], eps, _ptr(grad_scale)))
 

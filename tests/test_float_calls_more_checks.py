@@ -3,7 +3,7 @@ that records calls)."""
 import pytest
 import torch
 
-from test_float_calls_checks import _ran, niti            # noqa: F401  (the fixture)
+from test_float_calls_checks import _ran, _refused, niti            # noqa: F401  (the fixture)
 
 BF = torch.bfloat16
 
@@ -21,3 +21,20 @@ def test_parts_of_the_backward_call(niti):                          # noqa: F811
     for kw in (dict(dx=torch.zeros(3, 16, dtype=BF), need_dx=False), dict(dw=torch.zeros(5, 16), need_dw=False), dict(dbias=torch.zeros(5), need_dbias=False)):
         with pytest.raises(NitiError):
             niti.linear_act_bwd(a, s, w, s, d, **kw)
+
+
+def test_scalars_without_an_element_are_refused(niti):             # noqa: F811
+    """The pointer of an empty tensor is null, which the library takes for no gradient scale at all."""
+    p, g = torch.zeros(300), torch.zeros(300)
+    step, none = torch.ones(1, dtype=torch.int32), torch.empty(0, dtype=torch.int32)
+    plan = niti.adamw_tensors([p], [g], [p + 1], [p + 2])
+    w8 = torch.zeros(300, dtype=torch.int8)
+    _refused(niti, lambda: niti.adamw(plan, step, 1e-3, grad_scale=torch.empty(0)), lambda: niti.adamw(plan, none, 1e-3),
+             lambda: niti.adamw_tensors([p], [g], [p + 1], [p + 2], w8=[w8], s_w=[none]))
+    niti.adamw(plan, step, 1e-3, grad_scale=torch.ones(()))
+    assert len(_ran(niti, "niti_adamw")) == 1
+
+
+def test_weights_of_no_matrix_are_refused(niti):                    # noqa: F811
+    a, s = torch.zeros(3, 16, dtype=torch.int8), torch.zeros(1, dtype=torch.int32)
+    _refused(niti, lambda: niti.linear_act_fwd(a, s, torch.zeros((), dtype=torch.int8), s))
