@@ -753,6 +753,10 @@ class Niti:
                 self._scalar(sw, name + "s_w", torch.int32)
             array[i] = _AdamwTensor(_ptr(p), _ptr(g), _ptr(mi), _ptr(vi), _ptr(sm), _ptr(sv), _ptr(w), _ptr(sw), p.numel(),
                                     decay[i], _TYPES[g.dtype])
+        # (a parameter that is in the list twice would be updated by two blocks at once)
+        spans = sorted((x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()) for x in list(params) + [w for w in lists[5] if w is not None] if x.numel())
+        if any(a[1] > b[0] for a, b in zip(spans, spans[1:])):
+            raise NitiError(ERR_ARG, "adamw_tensors: two of the tensors share memory")
         return AdamwTensors(array, 8 if eight else 32, [list(params)] + lists)
 
     def adamw(self, tensors, step, lr, betas=(0.9, 0.999), eps=1e-8, grad_scale=None):

@@ -38,3 +38,16 @@ def test_scalars_without_an_element_are_refused(niti):             # noqa: F811
 def test_weights_of_no_matrix_are_refused(niti):                    # noqa: F811
     a, s = torch.zeros(3, 16, dtype=torch.int8), torch.zeros(1, dtype=torch.int32)
     _refused(niti, lambda: niti.linear_act_fwd(a, s, torch.zeros((), dtype=torch.int8), s))
+
+
+def test_parameters_that_share_memory_are_refused(niti):            # noqa: F811
+    """A list that holds a parameter twice would update it twice at once."""
+    p, g, w = torch.zeros(600), torch.zeros(600), torch.zeros(600, dtype=torch.int8)
+    sw = torch.zeros(1, dtype=torch.int32)
+    state = lambda n: [torch.zeros(n) for _ in range(2)]                                       # noqa: E731
+    m, v = state(300), state(300)
+    t = niti.adamw_tensors
+    _refused(niti, lambda: t([p, p], [g, g], state(600), state(600)), lambda: t([p[:300], p[299:599]], [g[:300]] * 2, m, v),
+             lambda: t([p[:300], p[300:]], [g[:300]] * 2, m, v, w8=[w[:300], w[100:400]], s_w=[sw, sw]))
+    # neighbours in one buffer, shared gradients and empty tensors are in order
+    t([p[:300], p[300:], p[:0]], [g[:300], g[:300], g[:0]], m + [p[:0]], v + [p[:0]], w8=[w[:300], w[300:], w[:0]], s_w=[sw] * 3)
