@@ -138,13 +138,26 @@ class _AdamwTensor(C.Structure):
 
 
 class AdamwTensors:
-    """The tensor list of ``Niti.adamw``: built once by ``Niti.adamw_tensors``, it holds the tensors it points to."""
+    """The tensor list of ``Niti.adamw``: built once by ``Niti.adamw_tensors``, it holds the tensors it points to.  A program whose
+    gradients get new storage in a step says so with ``set_grads``: the list would go on with the old ones."""
 
     def __init__(self, array, state_bits, tensors):
         self.array, self.state_bits, self.tensors = array, state_bits, tensors
 
     def __len__(self):
         return len(self.array)
+
+    def set_grads(self, grads):
+        """Points the list to other gradients (float32, bfloat16 or float16), for the calls that follow."""
+        grads, params = list(grads), self.tensors[0]
+        if len(grads) != len(params):
+            raise NitiError(ERR_ARG, "set_grads: one gradient per parameter")
+        for i, (g, p) in enumerate(zip(grads, params)):
+            if g is None or g.dtype not in _TYPES or g.shape != p.shape or g.device != p.device or not g.is_contiguous():
+                raise NitiError(ERR_ARG, "tensor %d: a contiguous gradient %s of float32, bfloat16 or float16 on %s is needed" % (i, tuple(p.shape), p.device))
+        for a, g in zip(self.array, grads):
+            a.g, a.g_type = g.data_ptr(), _TYPES[g.dtype]
+        self.tensors[1] = grads
 
 
 def _ptr(t):

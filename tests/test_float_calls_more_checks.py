@@ -51,3 +51,20 @@ def test_parameters_that_share_memory_are_refused(niti):            # noqa: F811
              lambda: t([p[:300], p[300:]], [g[:300]] * 2, m, v, w8=[w[:300], w[100:400]], s_w=[sw, sw]))
     # neighbours in one buffer, shared gradients and empty tensors are in order
     t([p[:300], p[300:], p[:0]], [g[:300], g[:300], g[:0]], m + [p[:0]], v + [p[:0]], w8=[w[:300], w[300:], w[:0]], s_w=[sw] * 3)
+
+
+def test_gradients_of_a_list_can_be_replaced(niti):                 # noqa: F811
+    from paper_2009_13108_b200 import NitiError
+    p, q = torch.zeros(300), torch.zeros(2, 5)
+    old = [torch.zeros(300), torch.zeros(2, 5)]
+    plan = niti.adamw_tensors([p, q], old, [p + 1, q + 1], [p + 2, q + 2])
+    new = [torch.zeros(300, dtype=BF), torch.zeros(2, 5)]
+    plan.set_grads(new)
+    assert [plan.array[i].g for i in (0, 1)] == [t.data_ptr() for t in new]
+    assert plan.array[0].g_type == 1 and plan.array[1].g_type == 0 and plan.tensors[1][0] is new[0]
+    for bad in ([new[0]], [new[0], torch.zeros(5, 2)], [new[0], torch.zeros(2, 5, dtype=torch.int32)], [new[0], torch.zeros(5, 2).t()],
+                [torch.zeros(300), torch.zeros(2, 5, device="meta")], [new[0], None]):
+        with pytest.raises(NitiError):
+            plan.set_grads(bad)
+        assert plan.array[0].g == new[0].data_ptr() and plan.tensors[1][1] is new[1]
+    niti.adamw(plan, torch.ones(1, dtype=torch.int32), 1e-3)

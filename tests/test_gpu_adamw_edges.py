@@ -129,3 +129,24 @@ def test_weights_that_are_not_finite_raise_the_status(niti, bits, w8, n, at):
         assert torch.isfinite(p[rest]).all() and not torch.isfinite(p[at])
         if w8:
             assert abs(int(w[at])) == 127
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_replaced_gradients_are_the_ones_used(niti, bits):
+    """A list whose gradients are replaced, by others of another type and alignment, goes on as a list built with them."""
+    n = 5000
+    first, second = torch.from_numpy(_gradients(n, 1, -4.0, -2.0)).cuda(), torch.from_numpy(_gradients(n + 1, 2, -4.0, -2.0)).cuda().to(torch.bfloat16)[1:]
+    runs = []
+    for replace in (False, True):
+        p = torch.from_numpy((0.05 * np.random.default_rng(8).standard_normal(n)).astype(F)).cuda()
+        m, v, s_m, s_v = niti.adamw_state(p, bits)
+        build = lambda g: niti.adamw_tensors([p], [g], [m], [v], s_m=[s_m] if bits == 8 else None, s_v=[s_v] if bits == 8 else None)      # noqa: E731
+        plan = build(first)
+        niti.adamw(plan, _step(1), LR)
+        if replace:
+            plan.set_grads([second])
+        else:
+            plan = build(second)
+        niti.adamw(plan, _step(2), LR)
+        runs.append((p, m, v))
+    assert all(torch.equal(a, b) for a, b in zip(*runs)) and niti.check() == 0
