@@ -10,7 +10,8 @@
  * headers of reduction scalars, see niti_begin_step()).  All work is enqueued on the
  * caller's stream (`stream` is a cudaStream_t passed as void*) and the calls
  * return without synchronising; one workspace must not be used by two calls
- * that can overlap on the GPU.
+ * that can overlap on the GPU.  The context's device is the current one when
+ * a call is made (niti_create() makes it that).
  *
  * Number format (Section 3.1): a tensor is an int8 payload plus ONE shared
  * exponent s, value = payload * 2^s.  Exponents and effective bit-widths live

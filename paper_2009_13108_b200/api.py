@@ -195,7 +195,10 @@ class Niti:
 
     # ---- helpers ----
     def _stream(self):
-        # (the raw handle: building a torch stream object took 2 us of a 12 us call)
+        # (the raw handle: building a torch stream object took 2 us of a 12 us call.  A default stream's handle names no device: a
+        # launch would run on the current one, with this one's memory)
+        if torch._C._cuda_getDevice() != self._gpu:
+            raise NitiError(ERR_ARG, "%s is not the current device" % self.device)
         return torch._C._cuda_getCurrentRawStream(self.device.index)
 
     def _ck(self, rc):

@@ -68,3 +68,17 @@ def test_gradients_of_a_list_can_be_replaced(niti):                 # noqa: F811
             plan.set_grads(bad)
         assert plan.array[0].g == new[0].data_ptr() and plan.tensors[1][1] is new[1]
     niti.adamw(plan, torch.ones(1, dtype=torch.int32), 1e-3)
+
+
+def test_another_current_device_is_refused(monkeypatch):
+    """A default stream belongs to the current device: a call there would run on one GPU with another's memory."""
+    from paper_2009_13108_b200 import Niti, NitiError
+    n = Niti.__new__(Niti)
+    n._gpu, n.device = 1, torch.device("cuda", 1)
+    current = [0]
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: current[0], raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 100 + d, raising=False)
+    with pytest.raises(NitiError, match="current device"):
+        n._stream()
+    current[0] = 1
+    assert n._stream() == 101
