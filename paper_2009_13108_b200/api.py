@@ -160,6 +160,15 @@ class AdamwTensors:
         self.tensors[1] = grads
 
 
+def _allocates(fn, gpu):
+    """Does torch's internal allocation function exist and answer as ``_new`` takes it to?"""
+    try:
+        t = fn((2, 3), (3, 1), torch.float16)
+        return t.get_device() == gpu and t.shape == (2, 3) and t.stride() == (3, 1) and t.dtype is torch.float16
+    except Exception:
+        return False
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -167,6 +176,7 @@ def _ptr(t):
 class Niti:
     """One library context on one CUDA device plus a growable workspace.  A program that captures calls into a graph keeps
     ``buffers()`` for as long as it replays it (``NitiTrainer.capture`` does)."""
+    _quick = False                         # outputs by torch's internal allocation function (see _new)
 
     def __init__(self, device: int = 0):
         if not torch.cuda.is_available():
@@ -180,6 +190,7 @@ class Niti:
             raise NitiError(rc, "niti_create failed (needs an sm_100 device)")
         self.h = h
         self._own_workspace(1 << 20)
+        self._quick = _allocates(_empty_on_current, device)
         self._ws_need = {}                 # workspace bytes of (op, dims) already asked for
 
     def close(self):
@@ -599,7 +610,7 @@ class Niti:
         """A new output, a matrix or a vector.  (torch.empty takes 2.4 us, torch.empty_strided 1.5, the allocation that torch's
         own generated code makes on the current device 0.8: of a small call's 10.)"""
         strides = (shape[1], 1) if len(shape) == 2 else (1,)
-        if _empty_on_current is not None and torch._C._cuda_getDevice() == self._gpu:
+        if self._quick and torch._C._cuda_getDevice() == self._gpu:
             return _empty_on_current(tuple(shape), strides, dtype)
         return torch.empty_strided(shape, strides, dtype=dtype, device=self.device)
 

@@ -82,3 +82,17 @@ def test_another_current_device_is_refused(monkeypatch):
         n._stream()
     current[0] = 1
     assert n._stream() == 101
+
+
+def test_an_allocator_that_answers_otherwise_is_not_used():
+    from paper_2009_13108_b200 import api
+    right = lambda shape, strides, dtype: torch.empty_strided(shape, strides, dtype=dtype)    # noqa: E731
+
+    def fails(*args):
+        raise TypeError("other arguments")
+
+    assert api._allocates(right, -1)
+    for wrong in (None, fails, lambda s, t, d: None, lambda s, t, d: right(s, t, torch.float32), lambda s, t, d: right(t, s, d),
+                  lambda s, t, d: right(s, (1, s[0]), d)):
+        assert not api._allocates(wrong, -1)
+    assert not api._allocates(right, 0)                                # (on another device)
