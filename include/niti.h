@@ -506,7 +506,7 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  *   m <- beta1 m + (1 - beta1) g,   v <- beta2 v + (1 - beta2) g^2,
  *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) m / (sqrt(v / (1 - beta2^t)) + eps),
  *   w8 <- floor(|p| 2^-s_w + 1/2), at most 127, sign of p (unless w8 is NULL): the int8 weights that the multiplies read,
- * with the exponent *s_w that the caller has chosen for the tensor.
+ * with the exponent *s_w that the caller has chosen for the tensor (clamped to -127 .. 127).
  * m and v are rounded to float32 after every product and sum (left to right, ((1 - beta2) g) g), so that codes are the
  * same wherever they are computed.
  * state_bits 32: m, v float32 [n].  state_bits 8: m and r = sqrt(v) are bytes in the format NITI_E4M3 with an int8

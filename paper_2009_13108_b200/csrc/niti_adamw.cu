@@ -412,7 +412,7 @@ adamw_kernel(const __grid_constant__ List<MOST> l, const Hyper hy, const int32_t
       known = lo;
       ready = -1;
       const int s_w = T.w8 ? *T.s_w : 0;
-      st.w_scale = niti_pow2(s_w < -126 ? 126 : s_w > 126 ? -126 : -s_w);
+      st.w_scale = s_w >= 127 ? __int_as_float(0x00400000) : niti_pow2(s_w < -127 ? 127 : -s_w);       // (2^-127 is subnormal)
       st.decay = T.decay;
     }
     const long long chunk0 = (long long)(gr - l.first[lo]) * group;

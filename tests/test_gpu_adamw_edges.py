@@ -150,3 +150,20 @@ def test_replaced_gradients_are_the_ones_used(niti, bits):
         niti.adamw(plan, _step(2), LR)
         runs.append((p, m, v))
     assert all(torch.equal(a, b) for a, b in zip(*runs)) and niti.check() == 0
+
+
+@pytest.mark.parametrize("n", [2048, 300])
+def test_int8_weights_at_the_ends_of_the_exponents(niti, n):
+    """floor(|p| 2^-s + 1/2) for the smallest and the largest exponents, of weights that are subnormal and nearly infinite (a
+    learning rate of zero leaves them as they are)."""
+    rng = np.random.default_rng(4)
+    small = np.ldexp(rng.uniform(1, 2, n), rng.integers(-149, -119, n)).astype(F)
+    large = np.ldexp(rng.uniform(1, 1.99, n), rng.integers(118, 128, n)).astype(F)
+    for s, p in [(-127, small), (-126, small), (-125, small), (125, large), (126, large), (127, large)]:
+        p = p * rng.choice([-1, 1], n).astype(F)
+        dev, w, z = torch.from_numpy(p).cuda(), torch.zeros(n, dtype=torch.int8, device="cuda"), torch.zeros(n, device="cuda")
+        niti.adamw(niti.adamw_tensors([dev], [z], [z.clone()], [z.clone()], w8=[w], s_w=[niti.scalar(s)]), _step(1), 0.0)
+        assert np.array_equal(dev.cpu().numpy(), p)
+        want = np.minimum(np.floor(np.abs(p.astype(float)) * 2.0 ** -s + 0.5), 127)
+        assert want.max() >= 2 and np.array_equal(w.cpu().numpy(), np.sign(p) * want), s
+    assert niti.check() == 0
