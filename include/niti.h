@@ -136,8 +136,9 @@ size_t niti_workspace_bytes(int op, const int64_t *dims, int ndims);
  * cores without the weights-resident mode of small-channel 3x3 convolutions,
  * 6 = automatic, but blocks that would wait for other blocks of their launch
  * leave their share to a later one at once.
- * 1-6 exist so that tests can cross-check the engines.  Returns the previous
- * value. */
+ * 1-6 exist so that tests can cross-check the engines.  The calls on float
+ * tensors do not look at it: niti_linear_act_fwd() and niti_linear_act_bwd() use
+ * the tensor cores whatever the engine.  Returns the previous value. */
 int niti_set_engine(niti_ctx *ctx, int engine);
 
 /* Number of kernels and memsets this context has enqueued so far. */
@@ -436,8 +437,8 @@ int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, cons
 /* ---- Float tensors at the boundary of the format: the feed-forward block of a transformer --------------------------
  * A residual stream of float rows (`type`: NITI_F32, NITI_BF16 or NITI_F16) enters the format through a norm, passes
  * int8 multiplies and comes back through their epilogue.  Float pointers are aligned to their element; rows of whole,
- * 16-byte aligned vectors are fastest.  M = 0 is a valid call (one exponent for the tensor is 0 then).  Sums, statistics and everything between a load and the
- * final rounding are float32.  No call of this section calls the hook of niti_set_reduce_hook(): an exponent for the tensor is
+ * 16-byte aligned vectors are fastest.  M = 0 is a valid call (one exponent for the tensor is 0 then).  Sums, statistics
+ * and everything between a load and the final rounding are float32.  No call of this section calls the hook of niti_set_reduce_hook(): an exponent for the tensor is
  * that of this process' rows.
  *
  * Rounding a float y to a payload with exponent s.  For a largest magnitude A the exponent is
@@ -517,8 +518,8 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * mix: x ^= x >> 16, x *= 0x7FEB352D, x ^= x >> 15, x *= 0x846CA68B, x ^= x >> 16 in 32 bits.  (To nearest, a state that
  * changes by a thousandth a step would stand still, and one that draws from its own discarded bits does where there is
  * no gradient: the same code times the same constant leaves the same bits.)
- * An element whose scaled gradient is not finite, or 2^63 or more, keeps its weight, m and v, and raises
- * NITI_DEV_NONFINITE; so does a weight that is not finite after the step (its int8 copy is +-127). */
+ * An element whose scaled gradient is not finite, or 2^63 or more, keeps its weight, m and v (8-bit ones are rounded
+ * again where their block's exponent changes), and raises NITI_DEV_NONFINITE; so does a weight that is not finite after the step (its int8 copy is +-127). */
 #define NITI_STATE_BLOCK 256
 typedef struct niti_adamw_tensor {
   float *p;
