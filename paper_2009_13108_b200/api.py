@@ -608,9 +608,10 @@ class Niti:
 
     def _new(self, shape, dtype):
         """A new output, a matrix or a vector.  (torch.empty takes 2.4 us, torch.empty_strided 1.5, the allocation that torch's
-        own generated code makes on the current device 0.8: of a small call's 10.)"""
+        own generated code makes on the current device 0.8: of a small call's 10.  That another device is current the call finds
+        when it asks for its stream.)"""
         strides = (shape[1], 1) if len(shape) == 2 else (1,)
-        if self._quick and torch._C._cuda_getDevice() == self._gpu:
+        if self._quick:
             return _empty_on_current(tuple(shape), strides, dtype)
         return torch.empty_strided(shape, strides, dtype=dtype, device=self.device)
 
