@@ -494,7 +494,8 @@ int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * The gradient of the residual is dout.  a has ONE exponent here (the sum over m cannot take out more); M and N at most
  * 131072.  dout, z and dx are of `type`, dw of dw_type; z may be NULL without an activation; dx, dw and dbias may be NULL;
  * dx may be the storage of dout or z.  round_mode 0 is refused where e has only the bits of a 16-bit type (no activation,
- * or NITI_ACT_RELU).  Workspace: NITI_OP_LINEAR_ACT_BWD. */
+ * or NITI_ACT_RELU).  act' of GELU is off by at most (2^-19 + z^2 2^-23) (Q(|z|) + |z| phi(z)), that of SiLU by 2^-20 (1 + |z|)
+ * times the sigmoid.  Workspace: NITI_OP_LINEAR_ACT_BWD. */
 int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, const int8_t *w,
                         const int32_t *s_w, const void *z, const void *dout, void *dx, void *dw, float *dbias, int type,
                         int dw_type, int M, int N, int K, int act, int round_mode, void *ws, size_t ws_bytes);

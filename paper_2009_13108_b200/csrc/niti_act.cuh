@@ -25,24 +25,35 @@ __device__ __forceinline__ float minus_magnitude(float z) {
   return r;
 }
 // The normal distribution's tail of two values -b >= 0: Q = 1 - Phi(-b) as q g with g = exp(-b^2 / 2).  q = Q exp(b^2 / 2) falls
-// slowly: with t = 1 / (1 - 0.265 b), q / t is a polynomial of degree 8 in b t, fitted on [0, 14] for the least relative error
-// (1.3e-8) with the value 1/2 at 0.  Relative to Q that leaves what reciprocal, exponential and roundings cost, at most 5 2^-22, and
-// the rounding of the exponent, b^2 2^-23.7 (measured 2.4e-7 up to 1, 5.4e-7 up to 3, 1.6e-6 up to 6).  Phi of a negative
-// argument is Q itself: 1 - (1 - Q) would leave no digits of a small tail.  (A shorter polynomial that only kept the absolute error
-// below 1e-7 took 6 us less of the two error passes of 4096 x 4096.)
+// slowly: with t = 1 / (1 - c b), q / t is a polynomial in b t, fitted on [0, 14] for the least relative error of Q (degree 8,
+// 1.3e-8), or, for the slope, where q stands beside |b| / sqrt(2 pi), of their sum (degree 6, 7e-8); its value at 0 is 1/2.
+// Relative to Q the first leaves what reciprocal, exponential and roundings cost, at most 5 2^-22, and the rounding of the
+// exponent, b^2 2^-23.7 (measured 2.4e-7 up to 1, 5.4e-7 up to 3, 1.6e-6 up to 6).  Phi of a negative argument is Q itself:
+// 1 - (1 - Q) would leave no digits of a small tail.  (A polynomial of degree 5 that only keeps Q's absolute error below 1e-7 took
+// 4 us less of the two error passes of 4096 x 4096, degree 8 there 2 us more.)
+template <bool SLOPE>
 __device__ __forceinline__ F2 normal_tail2(F2 b, F2 &g) {
   float d0, d1, x0, x1;
-  fma2(b, F2(-0.265f), F2(1.0f)).get(d0, d1);
+  fma2(b, F2(SLOPE ? -0.255f : -0.265f), F2(1.0f)).get(d0, d1);
   mul2(mul2(b, F2(-0.72134752f)), b).get(x0, x1);
   const F2 t(fast_reciprocal(d0), fast_reciprocal(d1)), s = mul2(b, t);
   g = F2(fast_exp2(x0), fast_exp2(x1));
-  F2 q = fma2(s, F2(7.47861634e-07f), F2(9.37091863e-06f));
-  q = fma2(s, q, F2(2.45498723e-05f));
-  q = fma2(s, q, F2(-0.000147059225f));
-  q = fma2(s, q, F2(-0.000331738207f));
-  q = fma2(s, q, F2(0.00898367632f));
-  q = fma2(s, q, F2(0.0736756772f));
-  q = fma2(s, q, F2(0.266442508f));
+  F2 q(0.0f);
+  if (SLOPE) {
+    q = fma2(s, F2(-2.25122367e-05f), F2(-0.00022684499f));
+    q = fma2(s, q, F2(-4.17664523e-06f));
+    q = fma2(s, q, F2(0.0112321274f));
+    q = fma2(s, q, F2(0.0790442675f));
+    q = fma2(s, q, F2(0.271441787f));
+  } else {
+    q = fma2(s, F2(7.47861634e-07f), F2(9.37091863e-06f));
+    q = fma2(s, q, F2(2.45498723e-05f));
+    q = fma2(s, q, F2(-0.000147059225f));
+    q = fma2(s, q, F2(-0.000331738207f));
+    q = fma2(s, q, F2(0.00898367632f));
+    q = fma2(s, q, F2(0.0736756772f));
+    q = fma2(s, q, F2(0.266442508f));
+  }
   q = fma2(s, q, F2(0.5f));
   return mul2(q, t);
 }
@@ -50,16 +61,17 @@ __device__ __forceinline__ F2 normal_tail2(F2 b, F2 &g) {
 __device__ __forceinline__ F2 gelu2(float z0, float z1) {
   const F2 b(minus_magnitude(z0), minus_magnitude(z1));
   F2 g(0.0f);
-  const F2 q = normal_tail2(b, g);
+  const F2 q = normal_tail2<false>(b, g);
   return fma2(b, mul2(q, g), F2(fmaxf(z0, 0.0f), fmaxf(z1, 0.0f)));
 }
-// Phi(z) + z phi(z): for negative z u = Q(|z|) - |z| phi(z), for others 1 - u: k u + (1 - k) / 2 with k = 1 or -1
+// Phi(z) + z phi(z): for negative z u = Q(|z|) - |z| phi(z), for others 1 - u
 __device__ __forceinline__ F2 gelu_slope2(float z0, float z1) {
   const F2 b(minus_magnitude(z0), minus_magnitude(z1));
   F2 g(0.0f);
-  const F2 q = normal_tail2(b, g);
-  const F2 u = mul2(fma2(b, F2(0.3989422804f), q), g), k(copysignf(1.0f, -z0), copysignf(1.0f, -z1));
-  return fma2(u, k, fma2(k, F2(-0.5f), F2(0.5f)));
+  const F2 q = normal_tail2<true>(b, g);
+  float u0, u1;
+  mul2(fma2(b, F2(0.3989422804f), q), g).get(u0, u1);
+  return F2(z0 < 0.0f ? u0 : 1.0f - u0, z1 < 0.0f ? u1 : 1.0f - u1);
 }
 __device__ __forceinline__ float gelu(float z) {
   float a, b;
