@@ -30,7 +30,7 @@ __device__ __forceinline__ float minus_magnitude(float z) {
 // Relative to Q the first leaves what reciprocal, exponential and roundings cost, at most 5 2^-22, and the rounding of the
 // exponent, b^2 2^-23.7 (measured 2.4e-7 up to 1, 5.4e-7 up to 3, 1.6e-6 up to 6).  Phi of a negative argument is Q itself:
 // 1 - (1 - Q) would leave no digits of a small tail.  (A polynomial of degree 5 that only keeps Q's absolute error below 1e-7 took
-// 4 us less of the two error passes of 4096 x 4096, degree 8 there 2 us more.)
+// 3 us less of the two error passes of 4096 x 4096, degree 8 there 2 us more.)
 template <bool SLOPE>
 __device__ __forceinline__ F2 normal_tail2(F2 b, F2 &g) {
   float d0, d1, x0, x1;

@@ -169,8 +169,9 @@ __device__ __forceinline__ void copy_kblock(const Params &p, const CUtensorMap *
 // other they left a seventh of them idle, twice, and each its first copies and its last epilogue uncovered: 4096 x 4096 x 1024
 // 19 + 19 -> 30 us, 2000 x 520 x 777 15 + 15 -> 17).
 // 8192 x 8192 x 8192 with bias, GELU, residual and z: 336 us alone, 3.27 POP/s, the tensor pipe busy for 90 % of it at the 1.5 GHz
-// that the power cap leaves; in a long run 420.  Short contractions are bound by the epilogue, about 9 instructions an element
-// without an activation and 15 with one: 4096 x 4096 x 1024 22 - 25 us, with eight epilogue warps instead of sixteen 26.
+// that the power cap leaves; in a long run 420 - 450.  Short contractions are bound by the epilogue, 11 instructions an
+// element without an activation, 20 with SiLU, 23 with GELU: 4096 x 4096 x 1024 23, 28 and 30 us (with eight epilogue warps instead
+// of sixteen 26 without one).
 // (Measured and left out: outputs through shared memory in whole 128-byte rows, 4096 x 4096 x 128 16 -> 16 us and 8192^3 365 ->
 // 400 for the stages that the buffers cost; copies by six threads instead of three, 11.7 -> 11.2 us at 64 x 4096 x 4096, slower
 // elsewhere; sums turned into floats by integer additions, 25 -> 27 us.)
@@ -701,9 +702,9 @@ struct ErrorGrid { int strips, rows, main; };
 
 // Largest |e| of the tensor, and the column sums of every block's rows; beside them, operands whose rows have to be padded for
 // the multiplies.  Bound: HBM and, with an activation, the exponentials and reciprocals of its slope (dout and z are read once
-// here; the rounding pass finds what fits of them in L2).  4096 x 4096 bfloat16 with GELU: 67 MB in 18 us from HBM, the
-// rounding pass 21 (one instance with the activation looked up for every element: 31 and 39; float32 instructions one by one
-// instead of in pairs: 19 and 24).  A pass that keeps e instead of computing it again would have to keep it in 32 bits, as many
+// here; the rounding pass finds what fits of them in L2).  4096 x 4096 bfloat16 with GELU: 67 MB in 18.5 us from HBM, the
+// rounding pass 22 where nothing is in L2; with SiLU 17 and 20.5 (one instance with the activation looked up for every element
+// took 31 and 39).  A pass that keeps e instead of computing it again would have to keep it in 32 bits, as many
 // bytes as both operands.
 template <int T, int VEC, int ACT>
 __global__ void __launch_bounds__(ERR_THREADS, 8)

@@ -291,7 +291,8 @@ norm_wide_kernel(const void *x, const void *res, const float *gain, void *h, int
 // in `part` and column_sum_kernel adds them up in a fixed order.  8192 x 4096 bfloat16 with dh: 268 MB in 42 us, 6.4 TB/s (0.99
 // of the measured copy rate), and 5 us for the sums of 296 blocks.
 // At most 16 columns of a thread in 16 bits: with 32 their operands, gains and sums do not fit 128 registers (4096 x 8192 bfloat16
-// as 256 threads of 32 columns took 513 us in spilled registers, as 512 of 16 it takes 57).
+// as 256 threads of 32 columns took 513 us in spilled registers, as 512 of 16 it takes 57).  float32 with 16 columns spills 80
+// bytes a thread.
 template <int T, int VEC, int NV>
 __global__ void __launch_bounds__(ROW_MOST, 1)
 norm_bwd_kernel(const void *dy, const void *h, const float *gain, const float *rstd, const void *dh, void *dx, float *part,
