@@ -438,8 +438,8 @@ int niti_maxpool2_bwd_idx(niti_ctx *ctx, void *stream, const int8_t *e_out, cons
  * A residual stream of float rows (`type`: NITI_F32, NITI_BF16 or NITI_F16) enters the format through a norm, passes
  * int8 multiplies and comes back through their epilogue.  Float pointers are aligned to their element; rows of whole,
  * 16-byte aligned vectors are fastest.  M = 0 is a valid call (one exponent for the tensor is 0 then).  Sums, statistics
- * and everything between a load and the final rounding are float32.  No call of this section calls the hook of niti_set_reduce_hook(): an exponent for the tensor is
- * that of this process' rows.
+ * and everything between a load and the final rounding are float32.  No call of this section calls the hook of
+ * niti_set_reduce_hook(): an exponent for the tensor is that of this process' rows.
  *
  * Rounding a float y to a payload with exponent s.  For a largest magnitude A the exponent is
  *   s = max(floor(log2 A) - 6, -100),  0 for A = 0,
@@ -483,7 +483,7 @@ int niti_dequantize(niti_ctx *ctx, void *stream, const void *q, const void *s, v
  * (NULL unless a backward pass follows) are of `type`; out may be the storage of the residual.  Exponents are clamped, and
  * NITI_DEV_EXP_RANGE raised, where s_a + s_w leaves [-128, 127].  With exponents per row a row's result depends on
  * nothing else.  GELU is max(z, 0) - |z| Q(|z|), the tail Q of the normal distribution being off by at most 2^-19 + z^2 2^-23 of
- * itself, SiLU by 2^-21; at infinite z both have their limits.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
+ * itself, SiLU by 2^-21 (numbers below 2^-118 may be 0); at infinite z both have their limits.  Workspace: NITI_OP_LINEAR_ACT_FWD. */
 int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, int row_exponents, const int8_t *w,
                         const int32_t *s_w, const float *bias, const void *residual, void *out, void *z, int type, int M,
                         int N, int K, int act, void *ws, size_t ws_bytes);
@@ -494,8 +494,8 @@ int niti_linear_act_fwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * The gradient of the residual is dout.  a has ONE exponent here (the sum over m cannot take out more); M and N at most
  * 131072.  dout, z and dx are of `type`, dw of dw_type; z may be NULL without an activation; dx, dw and dbias may be NULL;
  * dx may be the storage of dout or z.  round_mode 0 is refused where e has only the bits of a 16-bit type (no activation,
- * or NITI_ACT_RELU).  act' of GELU is off by at most (2^-19 + z^2 2^-23) (Q(|z|) + |z| phi(z)), that of SiLU by 2^-20 (1 + |z|)
- * times the sigmoid.  Workspace: NITI_OP_LINEAR_ACT_BWD. */
+ * or NITI_ACT_RELU).  Beside the rounding to float32, act' of GELU is off by at most (2^-19 + z^2 2^-23) (Q(|z|) + |z| phi(z)),
+ * that of SiLU by 2^-20 (1 + |z|) times the sigmoid.  Workspace: NITI_OP_LINEAR_ACT_BWD. */
 int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int32_t *s_a, const int8_t *w,
                         const int32_t *s_w, const void *z, const void *dout, void *dx, void *dw, float *dbias, int type,
                         int dw_type, int M, int N, int K, int act, int round_mode, void *ws, size_t ws_bytes);
@@ -520,7 +520,8 @@ int niti_linear_act_bwd(niti_ctx *ctx, void *stream, const int8_t *a, const int3
  * changes by a thousandth a step would stand still, and one that draws from its own discarded bits does where there is
  * no gradient: the same code times the same constant leaves the same bits.)
  * An element whose scaled gradient is not finite, or 2^63 or more, keeps its weight, m and v (8-bit ones are rounded
- * again where their block's exponent changes), and raises NITI_DEV_NONFINITE; so does a weight that is not finite after the step (its int8 copy is +-127). */
+ * again where their block's exponent changes), and raises NITI_DEV_NONFINITE; so does a weight that is not finite after
+ * the step (its int8 copy is +-127). */
 #define NITI_STATE_BLOCK 256
 typedef struct niti_adamw_tensor {
   float *p;
