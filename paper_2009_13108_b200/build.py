@@ -50,7 +50,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-o", LIB + ".tmp"]
+           "-shared", "-Xcompiler", "-fPIC", "--threads", str(min(len(SOURCES), os.cpu_count() or 1)), "-o", LIB + ".tmp"]
     if verbose:
         cmd += ["-Xptxas", "-v"]
     cmd += [os.path.join(CSRC, s) for s in SOURCES]
